@@ -409,6 +409,230 @@ fp8q_status fp8q_cast_f32(const float *x, int64_t n, float scale,
 fp8q_status fp8q_cast_f32_e5m2(const float *x, int64_t n, float scale,
                                uint8_t *codes, struct ihipStream_t *stream);
 
+/* ---- Operators around the FP8 linear layers --------------------------------
+ * What a policy's training step runs between its FP8 GEMMs: the norm that makes
+ * their operand, the gated feed-forward block, the weight gradients' operands
+ * from activations kept in 8 bits, and the policy loss from the logits. */
+
+/* The norm's weight is fp32 instead of bf16 (fp8q_rmsnorm and relatives). */
+enum { FP8Q_WEIGHT_F32 = 16u };
+
+/*
+ * Root-mean-square norm of the residual stream:
+ *   h = bf16(x + residual),  rstd = 1 / sqrt(mean over the row of h^2 + eps),
+ *   y = h rstd weight,
+ * in fp32, y rounded once.  The norm is that of the rounded h, which is what
+ * the backward pass is given.
+ *   x, residual  bf16 [rows][ldx], [rows][ldr]; residual may be null: then h is
+ *                x itself and the argument h must be null
+ *   weight       [cols], bf16, or fp32 with the flag FP8Q_WEIGHT_F32
+ *   h            bf16 [rows][ldh]; may be x or residual (same pointer and
+ *                leading dimension), else must not overlap them
+ *   rstd         fp32 [rows]
+ * fp8q_rmsnorm writes y in bf16 [rows][ldy]; y may not overlap any input.
+ * fp8q_rmsnorm_quantize writes y in 8 bits (Eq. 3 on the fp32 values): codes
+ * E4M3 [rows][ldc] and scales in the layout of fp8q_scales_count for g, which
+ * is FP8Q_BLOCK_1x128 or FP8Q_ROW (else FP8Q_ERR_UNSUPPORTED); flags: also
+ * FP8Q_POW2_SCALE.
+ * Shape rules: cols % 16 == 0 (% 128 for 1x128), cols <= 32768, rows below
+ * 2^22 (else FP8Q_ERR_UNSUPPORTED).  eps >= 0 (else FP8Q_ERR_INVAL).
+ * Alignment: x, residual, weight, h, y and codes 16-byte aligned, ldx, ldr, ldh
+ * and ldy multiples of 8, ldc of 16; rstd and scales 4-byte aligned.
+ */
+fp8q_status fp8q_rmsnorm(const void *x, int64_t ldx, const void *residual,
+                         int64_t ldr, const void *weight, unsigned flags,
+                         int64_t rows, int64_t cols, float eps, void *h,
+                         int64_t ldh, float *rstd, void *y, int64_t ldy,
+                         struct ihipStream_t *stream);
+fp8q_status fp8q_rmsnorm_quantize(const void *x, int64_t ldx,
+                                  const void *residual, int64_t ldr,
+                                  const void *weight, unsigned flags,
+                                  int64_t rows, int64_t cols, float eps,
+                                  void *h, int64_t ldh, float *rstd,
+                                  fp8q_granularity g, uint8_t *codes,
+                                  int64_t ldc, float *scales,
+                                  struct ihipStream_t *stream);
+
+/* Bytes of workspace fp8q_rmsnorm_backward needs; -1 for a size it refuses. */
+int64_t fp8q_rmsnorm_backward_workspace(int64_t rows, int64_t cols);
+
+/*
+ * Gradients of the norm.  With xhat = h rstd and g = dy weight,
+ *   dx = dres + rstd (g - xhat mean over the row of (g xhat)),
+ *   dweight = sum over the rows of dy xhat:
+ * dx is the gradient of x and of the residual alike.
+ *   dy, h   bf16 [rows][lddy], [rows][ldh] (h and rstd as the forward pass
+ *           wrote them); weight and flags as there
+ *   dres    bf16 [rows][ldres], the gradient that reaches h past the norm; may
+ *           be null (zero)
+ *   dx      bf16 [rows][lddx]; may be dy or dres (same pointer and leading
+ *           dimension)
+ *   dweight fp32 [cols], overwritten; the same on every run
+ * workspace: device memory of at least fp8q_rmsnorm_backward_workspace(rows,
+ * cols) bytes, 16-byte aligned, overwritten.  Shape and alignment rules: those
+ * of fp8q_rmsnorm; dweight 4-byte aligned.
+ */
+fp8q_status fp8q_rmsnorm_backward(const void *dy, int64_t lddy, const void *h,
+                                  int64_t ldh, const float *rstd,
+                                  const void *weight, unsigned flags,
+                                  const void *dres, int64_t ldres,
+                                  int64_t rows, int64_t cols, void *dx,
+                                  int64_t lddx, float *dweight,
+                                  void *workspace, int64_t workspace_bytes,
+                                  struct ihipStream_t *stream);
+
+/*
+ * The gated feed-forward block's first half, in one kernel:
+ *   G = X Wg^T,  U = X Wu^T,  H = silu(G) U,  silu(g) = g / (1 + exp(-g)),
+ * with X and the weights in 8 bits, as in fp8q_gemm's (1x128, 128x128) pair,
+ * fp32 sums, and H formed from the fp32 sums and rounded to bf16 once.
+ *   A    E4M3 [M][lda], sA 1x128 scales: X
+ *   B    E4M3 [2 F][ldb], sB 128x128 scales: the F rows of Wg, then those of
+ *        Wu (fp8q_quantize of the two weights one below the other)
+ *   H    bf16 [M][ldh]
+ *   pre  bf16 [M][ldp], G in columns 0 .. F-1 and U in F .. 2F-1, for the
+ *        backward pass; may be null
+ * fp8q_gemm_gated_quantized writes H in 8 bits, for the down projection:
+ * exactly fp8q_quantize(H, M, F, F, FP8Q_BLOCK_1x128, 0, codes, ldq, scales) of
+ * the H that fp8q_gemm_gated computes; codes E4M3 [M][ldq], scales
+ * [F/128][M].
+ * Shape rules: K % 128 == 0, F % 128 == 0; 2 F ldb below 2^31, M K / 128 below
+ * 2^29 and at most 2^22 tiles of 128 x 64 outputs (else FP8Q_ERR_UNSUPPORTED).  Alignment: A, B and codes 16-byte aligned, lda, ldb
+ * and ldq multiples of 16; H and pre 8-byte aligned with ldh and ldp multiples
+ * of 4; scales 4-byte aligned.  The outputs must not overlap each other or an
+ * input.
+ */
+fp8q_status fp8q_gemm_gated(const uint8_t *A, const float *sA, int64_t lda,
+                            const uint8_t *B, const float *sB, int64_t ldb,
+                            int64_t M, int64_t F, int64_t K, void *H,
+                            int64_t ldh, void *pre, int64_t ldp,
+                            struct ihipStream_t *stream);
+fp8q_status fp8q_gemm_gated_quantized(const uint8_t *A, const float *sA,
+                                      int64_t lda, const uint8_t *B,
+                                      const float *sB, int64_t ldb, int64_t M,
+                                      int64_t F, int64_t K, void *pre,
+                                      int64_t ldp, uint8_t *codes, int64_t ldq,
+                                      float *scales,
+                                      struct ihipStream_t *stream);
+
+/*
+ * Backward pass of H = silu(G) U from dH and the kept pre-activations:
+ *   s = 1 / (1 + exp(-G)),  dG = dH U s (1 + G (1 - s)),  dU = dH G s,
+ * in fp32, quantized once, as one matrix D = [dG | dU] of 2 F columns in both
+ * layouts of the backward GEMMs (those of fp8q_quantize_dual):
+ *   codes_r, scales_r  [M][ldr] and [2F/128][M], per 1x128 unit: the data
+ *                      gradient dX = D W (its K is 2 F)
+ *   codes_t, scales_t  [2F][ldt] and [Mp/128][2F], transposed, per 128 rows:
+ *                      the weight gradients [dWg; dWu] = D^T X (its K is Mp)
+ * where Mp is M rounded up to a multiple of 128; columns M .. Mp-1 of codes_t
+ * are written as zeros.
+ *   dh   bf16 [M][lddh];  pre  bf16 [M][ldp] as fp8q_gemm_gated wrote it
+ * flags: FP8Q_E5M2, FP8Q_POW2_SCALE, both, or 0.  Shape rules: F % 128 == 0, M
+ * <= 65535 x 128 (else FP8Q_ERR_UNSUPPORTED).  Alignment: dh, pre and both
+ * code arrays 16-byte aligned, lddh and ldp multiples of 8, ldr and ldt of 16
+ * (ldt >= Mp); scales 4-byte aligned.  The outputs must not overlap.
+ */
+fp8q_status fp8q_gated_backward(const void *dh, int64_t lddh, const void *pre,
+                                int64_t ldp, int64_t M, int64_t F,
+                                unsigned flags, uint8_t *codes_r, int64_t ldr,
+                                float *scales_r, uint8_t *codes_t, int64_t ldt,
+                                float *scales_t, struct ihipStream_t *stream);
+
+/*
+ * An activation kept in 8 bits as the weight gradient's operand: from the codes
+ * and 1x128 scales that a forward GEMM took, the transposed codes in units of
+ * 128 rows.  With v = RN32(S code) for every element, S' = RN32(amax of |v|
+ * over 128 rows of a column / 448) (1 when that is 0) and codes_t[c][r] the E4M3
+ * value nearest to v / S'; flags: FP8Q_POW2_SCALE (for S') or 0.
+ *   codes    E4M3 [rows][ldc], scales [cols/128][rows]
+ *   codes_t  E4M3 [cols][ldt], ldt >= Rp, rows rounded up to a multiple of
+ *            128; columns rows .. Rp-1 are written as zeros
+ *   scales_t [Rp/128][cols]
+ * Shape rules: cols % 128 == 0, rows <= 65535 x 128 (else
+ * FP8Q_ERR_UNSUPPORTED).  Alignment: both code arrays 16-byte aligned, ldc and
+ * ldt multiples of 16; scales 4-byte aligned.  codes must not hold NaN.
+ */
+fp8q_status fp8q_requantize_transposed(const uint8_t *codes, int64_t ldc,
+                                       const float *scales, int64_t rows,
+                                       int64_t cols, unsigned flags,
+                                       uint8_t *codes_t, int64_t ldt,
+                                       float *scales_t,
+                                       struct ihipStream_t *stream);
+
+/* Types of the logits. */
+typedef enum { FP8Q_BF16 = 0, FP8Q_F32 = 1 } fp8q_dtype;
+
+/*
+ * Bytes of workspace the two calls below need for T tokens over a vocabulary of
+ * V; -1 for a size they refuse.
+ */
+int64_t fp8q_policy_loss_workspace(int64_t T, int64_t V);
+
+/*
+ * Log-probabilities of the taken tokens: over each row of logits x (bf16 or
+ * fp32, [T][ld]), with z = x / temperature,
+ *   logp = z[token] - log sum exp(z),  entropy = -sum p log p, p = softmax(z),
+ * fp32 [T] each.  A token outside 0 .. V-1 is not in the vocabulary: its row is
+ * not read and both are 0.  Logits of -inf have probability 0; a row of NaN, of
+ * +inf or of nothing but -inf gives NaN.
+ * workspace: at least fp8q_policy_loss_workspace(T, V) bytes, 16-byte aligned,
+ * overwritten (calls that share one must be ordered).  Shape rules: T below
+ * 2^22, V below 2^31 (else FP8Q_ERR_UNSUPPORTED).  Alignment: logits to their type's
+ * size (any ld >= V), tokens 8-byte, the others 4-byte aligned.
+ * temperature > 0 (else FP8Q_ERR_INVAL).
+ */
+fp8q_status fp8q_token_logprobs(const void *logits, fp8q_dtype dtype,
+                                int64_t T, int64_t V, int64_t ld,
+                                const int64_t *tokens, double temperature,
+                                float *logp, float *entropy, void *workspace,
+                                int64_t workspace_bytes,
+                                struct ihipStream_t *stream);
+
+/* One batch for fp8q_policy_loss: per-token fp32 arrays of T entries on the
+ * device, and the loss's constants. */
+typedef struct fp8q_policy_batch {
+  const int64_t *tokens;  /* the taken tokens                                  */
+  const float *logp_old;  /* their log-probabilities under the old policy      */
+  const float *adv;       /* advantages A                                      */
+  const float *weight;    /* c: each token's weight in the loss; 0 outside the
+                             response                                           */
+  const float *w_tis;     /* truncated importance weights w; null: 1           */
+  const float *logp_ref;  /* log-probabilities under the reference policy;
+                             null: no KL term                                   */
+  const fp8q_clip_result *clip; /* bounds l_new and h_new, on the device, as
+                             fp8q_calibrate_clip writes them; null: the next two */
+  double clip_low, clip_high;   /* bounds of the ratio                          */
+  double beta;                  /* weight of the KL term                        */
+  double temperature;           /* the logits are divided by it                 */
+} fp8q_policy_batch;
+
+/*
+ * The clipped policy loss with truncated importance sampling (Eq. 4) and a KL
+ * term, and its gradient in the logits, from one read of them.  With logp and
+ * entropy as fp8q_token_logprobs gives them, r = exp(logp - logp_old), d =
+ * logp_ref - logp:
+ *   l = -w min(r A, clip(r, low, high) A) + beta (exp(d) - d - 1),
+ *   loss = sum over the tokens of c l,
+ *   dlogits[t][j] = c l' / temperature (delta(j = token) - p_j),
+ *   l' = -w A r where r A <= clip(r, low, high) A, else 0, + beta (1 - exp(d)).
+ * Rows whose weight is 0 or whose token is outside the vocabulary are not read
+ * (they may hold anything): their logp, entropy and gradient are 0.
+ *   loss     fp32 [1]
+ *   dlogits  [T][ldd], the logits' type; may be the logits (same pointer and
+ *            leading dimension), else must not overlap them
+ * batch (a HOST pointer, read during the call).  Errors, workspace, shape and
+ * alignment rules: those of fp8q_token_logprobs; bounds that are not ordered
+ * (clip_low > clip_high, or NaN), beta NaN -> FP8Q_ERR_INVAL.  Results are the
+ * same on every run.
+ */
+fp8q_status fp8q_policy_loss(const void *logits, fp8q_dtype dtype, int64_t T,
+                             int64_t V, int64_t ld,
+                             const fp8q_policy_batch *batch, float *loss,
+                             void *dlogits, int64_t ldd, float *logp,
+                             float *entropy, void *workspace,
+                             int64_t workspace_bytes,
+                             struct ihipStream_t *stream);
+
 /* Static string naming a status. */
 const char *fp8q_status_string(fp8q_status status);
 

@@ -26,6 +26,7 @@ TENSOR, ROW, COL, BLOCK_1x128, BLOCK_128x1, BLOCK_128x128 = range(6)
 OUT_TRANSPOSED = 1
 POW2_SCALE = 2
 E5M2 = 4                      # quantize flag: E5M2 codes (F_max = 57344)
+WEIGHT_F32 = 16               # norm flag: its weight is fp32
 A_E5M2, B_E5M2 = 1, 2         # gemm_formats operand formats
 _STATUS = {0: "FP8Q_OK", -1: "FP8Q_ERR_INVAL", -2: "FP8Q_ERR_UNSUPPORTED",
            -3: "FP8Q_ERR_ALIGN", -4: "FP8Q_ERR_HIP"}
@@ -35,7 +36,10 @@ EXPORTS = ("fp8q_scales_count", "fp8q_quantize", "fp8q_quantize_dual",
            "fp8q_gemm_splitk_workspace", "fp8q_gemm_splitk",
            "fp8q_calibrate_clip_workspace", "fp8q_calibrate_clip", "fp8q_calibrate_clip_noalloc",
            "fp8q_cast_f32",
-           "fp8q_cast_f32_e5m2", "fp8q_status_string")
+           "fp8q_cast_f32_e5m2", "fp8q_rmsnorm", "fp8q_rmsnorm_quantize", "fp8q_rmsnorm_backward_workspace",
+           "fp8q_rmsnorm_backward", "fp8q_gemm_gated", "fp8q_gemm_gated_quantized", "fp8q_gated_backward",
+           "fp8q_requantize_transposed", "fp8q_policy_loss_workspace", "fp8q_token_logprobs", "fp8q_policy_loss",
+           "fp8q_status_string")
 
 
 MAX_GROUP = 8
@@ -63,6 +67,12 @@ class ClipResult(ctypes.Structure):
                    ("l_updated", ctypes.c_int32), ("h_updated", ctypes.c_int32)])
 
 
+class PolicyBatch(ctypes.Structure):
+    """fp8q_policy_batch (include/fp8q.h)."""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("tokens", "logp_old", "adv", "weight", "w_tis", "logp_ref", "clip")]
+                + [(n, ctypes.c_double) for n in ("clip_low", "clip_high", "beta", "temperature")])
+
+
 _CLIP_FIELDS = tuple(n for n, _ in ClipResult._fields_)
 _CLIP_STRUCT = struct.Struct("=7d2q2i")
 
@@ -83,7 +93,10 @@ _calls = None
 # the entry points of binding.cpp's Api, in its order
 _NATIVE_API = ("fp8q_scales_count", "fp8q_quantize", "fp8q_quantize_dual", "fp8q_gemm_formats", "fp8q_gemm_grouped",
                "fp8q_gemm_pow2", "fp8q_gemm_quantized", "fp8q_gemm_splitk_workspace", "fp8q_gemm_splitk",
-               "fp8q_calibrate_clip_workspace", "fp8q_calibrate_clip")
+               "fp8q_calibrate_clip_workspace", "fp8q_calibrate_clip", "fp8q_rmsnorm", "fp8q_rmsnorm_quantize",
+               "fp8q_rmsnorm_backward_workspace", "fp8q_rmsnorm_backward", "fp8q_gemm_gated",
+               "fp8q_gemm_gated_quantized", "fp8q_gated_backward", "fp8q_requantize_transposed",
+               "fp8q_policy_loss_workspace", "fp8q_token_logprobs", "fp8q_policy_loss")
 
 
 def lib():
@@ -131,6 +144,29 @@ def lib():
         L.fp8q_cast_f32_e5m2.argtypes = [p, i64, ctypes.c_float, p, p]
         L.fp8q_cast_f32_e5m2.restype = i32
         L.fp8q_cast_f32.restype = i32
+        f32 = ctypes.c_float
+        L.fp8q_rmsnorm.argtypes = [p, i64, p, i64, p, u32, i64, i64, f32, p, i64, p, p, i64, p]
+        L.fp8q_rmsnorm.restype = i32
+        L.fp8q_rmsnorm_quantize.argtypes = [p, i64, p, i64, p, u32, i64, i64, f32, p, i64, p, i32, p, i64, p, p]
+        L.fp8q_rmsnorm_quantize.restype = i32
+        L.fp8q_rmsnorm_backward_workspace.argtypes = [i64, i64]
+        L.fp8q_rmsnorm_backward_workspace.restype = i64
+        L.fp8q_rmsnorm_backward.argtypes = [p, i64, p, i64, p, p, u32, p, i64, i64, i64, p, i64, p, p, i64, p]
+        L.fp8q_rmsnorm_backward.restype = i32
+        L.fp8q_gemm_gated.argtypes = [p, p, i64, p, p, i64, i64, i64, i64, p, i64, p, i64, p]
+        L.fp8q_gemm_gated.restype = i32
+        L.fp8q_gemm_gated_quantized.argtypes = [p, p, i64, p, p, i64, i64, i64, i64, p, i64, p, i64, p, p]
+        L.fp8q_gemm_gated_quantized.restype = i32
+        L.fp8q_gated_backward.argtypes = [p, i64, p, i64, i64, i64, u32, p, i64, p, p, i64, p, p]
+        L.fp8q_gated_backward.restype = i32
+        L.fp8q_requantize_transposed.argtypes = [p, i64, p, i64, i64, u32, p, i64, p, p]
+        L.fp8q_requantize_transposed.restype = i32
+        L.fp8q_policy_loss_workspace.argtypes = [i64, i64]
+        L.fp8q_policy_loss_workspace.restype = i64
+        L.fp8q_token_logprobs.argtypes = [p, i32, i64, i64, i64, p, d, p, p, p, i64, p]
+        L.fp8q_token_logprobs.restype = i32
+        L.fp8q_policy_loss.argtypes = [p, i32, i64, i64, i64, ctypes.POINTER(PolicyBatch), p, p, i64, p, p, p, i64, p]
+        L.fp8q_policy_loss.restype = i32
         L.fp8q_status_string.argtypes = [i32]
         L.fp8q_status_string.restype = ctypes.c_char_p
         native.bind(tuple(ctypes.cast(getattr(L, n), p).value for n in _NATIVE_API))
@@ -504,3 +540,269 @@ def cast_f32(x, scale, codes=None, e5m2=False):
     st = fn(x.data_ptr(), x.numel(), float(scale), codes.data_ptr(), _stream(x))
     _check(st, "fp8q_cast_f32_e5m2" if e5m2 else "fp8q_cast_f32")
     return codes
+
+
+def _given(t, dtype, what, shape, device):
+    """The output t checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return _matrix(t, dtype, what, shape, device)
+
+
+def _new_vector(t, dtype, n, what, device):
+    """The vector t checked, or a new one of n elements."""
+    return torch.empty(n, dtype=dtype, device=device) if t is None else _vector(t, dtype, n, what, device)
+
+
+def _norm_weight(weight, cols, device):
+    """The norm's weight checked, and its flag."""
+    if not isinstance(weight, torch.Tensor) or weight.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("weight must be a bfloat16 or float32 tensor")
+    _vector(weight, weight.dtype, cols, "weight", device)
+    if weight.dim() != 1 or weight.numel() != cols:
+        raise ValueError("weight must have one element per column")
+    return WEIGHT_F32 if weight.dtype == torch.float32 else 0
+
+
+def _norm_inputs(x, weight, residual, h, rstd):
+    """The checks and outputs that both norms share: (flag, h, rstd, the C
+    arguments for the residual and for h)."""
+    _matrix(x, torch.bfloat16, "x")
+    rows, cols = x.shape
+    flag = _norm_weight(weight, cols, x.device)
+    rstd = _new_vector(rstd, torch.float32, rows, "rstd", x.device)
+    if residual is None:
+        if h is not None:
+            raise ValueError("h is x itself without a residual")
+        return flag, x, rstd, (None, 0), (None, 0)
+    _matrix(residual, torch.bfloat16, "residual", x.shape, x.device)
+    h = _given(h, torch.bfloat16, "h", (rows, cols), x.device)
+    return flag, h, rstd, (residual.data_ptr(), _ld(residual)), (h.data_ptr(), _ld(h))
+
+
+def rmsnorm(x, weight, eps, residual=None, out=None, h=None, rstd=None):
+    """RMS norm of a bf16 CUDA tensor x[rows, cols], or of h = bf16(x +
+    residual): returns (y, h, rstd), y = h rstd weight in bf16, h the new
+    residual stream (x itself without a residual; `h` may be x or residual)
+    and rstd fp32 [rows], which rmsnorm_backward takes.  weight: bf16 or fp32
+    [cols]."""
+    r = _fast().rmsnorm(x, weight, eps, residual, out, h, rstd)
+    if r is not None:
+        return _done(r, "fp8q_rmsnorm")
+    flag, h, rstd, res, ho = _norm_inputs(x, weight, residual, h, rstd)
+    out = _given(out, torch.bfloat16, "out", tuple(x.shape), x.device)
+    st = lib().fp8q_rmsnorm(x.data_ptr(), _ld(x), *res, weight.data_ptr(), flag, *x.shape, float(eps), *ho,
+                            rstd.data_ptr(), out.data_ptr(), _ld(out), _stream(x))
+    _check(st, "fp8q_rmsnorm")
+    return out, h, rstd
+
+
+def rmsnorm_quantize(x, weight, eps, granularity=BLOCK_1x128, residual=None, pow2=False, codes=None, scales=None,
+                     h=None, rstd=None):
+    """rmsnorm() with y in 8 bits, quantized from its fp32 values: returns
+    (codes, scales, h, rstd), codes and scales as quantize() gives them for
+    `granularity` (BLOCK_1x128 or ROW), a GEMM's operand."""
+    flags = POW2_SCALE if pow2 else 0
+    r = _fast().rmsnorm_quantize(x, weight, eps, granularity, flags, residual, codes, scales, h, rstd)
+    if r is not None:
+        return _done(r, "fp8q_rmsnorm_quantize")
+    flag, h, rstd, res, ho = _norm_inputs(x, weight, residual, h, rstd)
+    rows, cols = x.shape
+    codes = _given(codes, torch.uint8, "codes", (rows, cols), x.device)
+    scales = _new_vector(scales, torch.float32, scales_count(rows, cols, granularity), "scales", x.device)
+    st = lib().fp8q_rmsnorm_quantize(x.data_ptr(), _ld(x), *res, weight.data_ptr(), flag | flags, rows, cols,
+                                     float(eps), *ho, rstd.data_ptr(), granularity, codes.data_ptr(), _ld(codes),
+                                     scales.data_ptr(), _stream(x))
+    _check(st, "fp8q_rmsnorm_quantize")
+    return codes, scales, h, rstd
+
+
+def rmsnorm_backward(dy, h, rstd, weight, dres=None, dx=None, dweight=None, workspace=None):
+    """Gradients of rmsnorm() from that of y, with h and rstd as it returned
+    them and `dres` the gradient that reaches h past the norm: returns (dx,
+    dweight), dx in bf16 the gradient of x and of the residual alike (`dx`
+    may be dy or dres), dweight fp32 [cols].  workspace: a uint8 CUDA tensor
+    of fp8q_rmsnorm_backward_workspace bytes (a new one when None)."""
+    r = _fast().rmsnorm_backward(dy, h, rstd, weight, dres, dx, dweight, workspace)
+    if r is not None:
+        return _done(r, "fp8q_rmsnorm_backward")
+    _matrix(dy, torch.bfloat16, "dy")
+    rows, cols = dy.shape
+    dev = dy.device
+    _matrix(h, torch.bfloat16, "h", dy.shape, dev)
+    _vector(rstd, torch.float32, rows, "rstd", dev)
+    flag = _norm_weight(weight, cols, dev)
+    if dres is not None:
+        _matrix(dres, torch.bfloat16, "dres", dy.shape, dev)
+    dx = _given(dx, torch.bfloat16, "dx", (rows, cols), dev)
+    dweight = _new_vector(dweight, torch.float32, cols, "dweight", dev)
+    need = max(lib().fp8q_rmsnorm_backward_workspace(rows, cols), 0)
+    workspace = _new_vector(workspace, torch.uint8, max(need, 16), "workspace", dev)
+    st = lib().fp8q_rmsnorm_backward(dy.data_ptr(), _ld(dy), h.data_ptr(), _ld(h), rstd.data_ptr(), weight.data_ptr(),
+                                     flag, None if dres is None else dres.data_ptr(), 0 if dres is None else _ld(dres),
+                                     rows, cols, dx.data_ptr(), _ld(dx), dweight.data_ptr(), workspace.data_ptr(),
+                                     workspace.numel(), _stream(dy))
+    _check(st, "fp8q_rmsnorm_backward")
+    return dx, dweight
+
+
+def _gated_operands(a, sa, b, sb, save, pre):
+    """The checks that both gated GEMMs share: (M, F, K, pre, its C arguments)."""
+    M, N, K = _operands(a, sa, BLOCK_1x128, b, sb, BLOCK_128x128)
+    if N % 2:
+        raise ValueError("b holds the rows of two weights")
+    if save or pre is not None:
+        pre = _given(pre, torch.bfloat16, "pre", (M, N), a.device)
+        return M, N // 2, K, pre, (pre.data_ptr(), _ld(pre))
+    return M, N // 2, K, None, (None, 0)
+
+
+def gemm_gated(a, sa, b, sb, save=False, out=None, pre=None):
+    """H = silu(X Wg^T) * (X Wu^T) in one kernel, for a gated feed-forward
+    block on FP8 operands: a, sa the codes and 1x128 scales of X [M, K]; b, sb
+    those of the two weights one below the other, [2 F, K] with 128x128
+    scales.  Returns (h, pre): h bf16 [M, F]; pre the pre-activations [M, 2 F]
+    (gate, then up) for gated_backward when `save` (or given), else None."""
+    r = _fast().gemm_gated(a, sa, b, sb, save, out, pre)
+    if r is not None:
+        return _done(r, "fp8q_gemm_gated")
+    M, F, K, pre, pc = _gated_operands(a, sa, b, sb, save, pre)
+    out = _given(out, torch.bfloat16, "out", (M, F), a.device)
+    st = lib().fp8q_gemm_gated(a.data_ptr(), sa.data_ptr(), _ld(a), b.data_ptr(), sb.data_ptr(), _ld(b), M, F, K,
+                               out.data_ptr(), _ld(out), *pc, _stream(a))
+    _check(st, "fp8q_gemm_gated")
+    return out, pre
+
+
+def gemm_gated_quantized(a, sa, b, sb, save=False, codes=None, scales=None, pre=None):
+    """gemm_gated() with H in 8 bits, the down projection's operand: returns
+    (codes, scales, pre), exactly quantize(h, BLOCK_1x128) of its h."""
+    r = _fast().gemm_gated_quantized(a, sa, b, sb, save, codes, scales, pre)
+    if r is not None:
+        return _done(r, "fp8q_gemm_gated_quantized")
+    M, F, K, pre, pc = _gated_operands(a, sa, b, sb, save, pre)
+    codes = _given(codes, torch.uint8, "codes", (M, F), a.device)
+    scales = _new_vector(scales, torch.float32, scales_count(M, F, BLOCK_1x128), "scales", a.device)
+    st = lib().fp8q_gemm_gated_quantized(a.data_ptr(), sa.data_ptr(), _ld(a), b.data_ptr(), sb.data_ptr(), _ld(b), M, F,
+                                         K, *pc, codes.data_ptr(), _ld(codes), scales.data_ptr(), _stream(a))
+    _check(st, "fp8q_gemm_gated_quantized")
+    return codes, scales, pre
+
+
+def _padded(rows):
+    """rows rounded up to whole units of 128."""
+    return (rows + 127) // 128 * 128
+
+
+def gated_backward(dh, pre, pow2=False, e5m2=False, codes_r=None, scales_r=None, codes_t=None, scales_t=None):
+    """Gradients of gemm_gated()'s pre-activations from that of h, as the FP8
+    operands of the backward GEMMs: D = [dG | dU], M x 2 F.  Returns
+    (codes_r, scales_r, codes_t, scales_t): D per 1x128 unit, for dX = D W,
+    and D^T per 128x1 unit, [2 F, Mp], for [dWg; dWu] = D^T X, Mp being M
+    rounded up to a multiple of 128 (zeros there).  pow2, e5m2: as in
+    quantize()."""
+    flags = (POW2_SCALE if pow2 else 0) | (E5M2 if e5m2 else 0)
+    r = _fast().gated_backward(dh, pre, flags, codes_r, scales_r, codes_t, scales_t)
+    if r is not None:
+        return _done(r, "fp8q_gated_backward")
+    _matrix(dh, torch.bfloat16, "dh")
+    M, F = dh.shape
+    dev = dh.device
+    _matrix(pre, torch.bfloat16, "pre", (M, 2 * F), dev)
+    codes_r = _given(codes_r, torch.uint8, "codes_r", (M, 2 * F), dev)
+    codes_t = _given(codes_t, torch.uint8, "codes_t", (2 * F, _padded(M)), dev)
+    scales_r = _new_vector(scales_r, torch.float32, M * (2 * F // 128), "scales_r", dev)
+    scales_t = _new_vector(scales_t, torch.float32, _padded(M) // 128 * 2 * F, "scales_t", dev)
+    st = lib().fp8q_gated_backward(dh.data_ptr(), _ld(dh), pre.data_ptr(), _ld(pre), M, F, flags, codes_r.data_ptr(),
+                                   _ld(codes_r), scales_r.data_ptr(), codes_t.data_ptr(), _ld(codes_t),
+                                   scales_t.data_ptr(), _stream(dh))
+    _check(st, "fp8q_gated_backward")
+    return codes_r, scales_r, codes_t, scales_t
+
+
+def requantize_transposed(codes, scales, pow2=False, codes_t=None, scales_t=None):
+    """The weight gradient's operand from an activation kept in 8 bits: codes
+    [rows, cols] (E4M3) with 1x128 scales in, (codes_t, scales_t) out, the
+    transpose [cols, Rp] per 128x1 unit, Rp being rows rounded up to a
+    multiple of 128 (zeros there).  pow2: power-of-two scales."""
+    r = _fast().requantize_transposed(codes, scales, POW2_SCALE if pow2 else 0, codes_t, scales_t)
+    if r is not None:
+        return _done(r, "fp8q_requantize_transposed")
+    _matrix(codes, torch.uint8, "codes")
+    rows, cols = codes.shape
+    dev = codes.device
+    _vector(scales, torch.float32, scales_count(rows, cols, BLOCK_1x128), "scales", dev)
+    codes_t = _given(codes_t, torch.uint8, "codes_t", (cols, _padded(rows)), dev)
+    scales_t = _new_vector(scales_t, torch.float32, _padded(rows) // 128 * cols, "scales_t", dev)
+    st = lib().fp8q_requantize_transposed(codes.data_ptr(), _ld(codes), scales.data_ptr(), rows, cols,
+                                          POW2_SCALE if pow2 else 0, codes_t.data_ptr(), _ld(codes_t),
+                                          scales_t.data_ptr(), _stream(codes))
+    _check(st, "fp8q_requantize_transposed")
+    return codes_t, scales_t
+
+
+def _logits(logits, tokens, workspace):
+    """The checks that the two calls on logits share: (their type's code, T, V,
+    workspace)."""
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be a 2-D bfloat16 or float32 CUDA tensor")
+    _matrix(logits, logits.dtype, "logits")
+    T, V = logits.shape
+    _vector(tokens, torch.int64, T, "tokens", logits.device)
+    need = lib().fp8q_policy_loss_workspace(T, V)
+    if need < 0:
+        raise ValueError("invalid number of tokens or vocabulary size")
+    return 1 if logits.dtype == torch.float32 else 0, T, V, _new_vector(workspace, torch.uint8, need, "workspace",
+                                                                        logits.device)
+
+
+def token_logprobs(logits, tokens, temperature=1.0, logp=None, entropy=None, workspace=None):
+    """Log-probabilities of `tokens` (int64 [T]) under softmax(logits /
+    temperature), logits bf16 or fp32 [T, V], and the rows' entropies: returns
+    (logp, entropy), fp32 [T].  A token outside the vocabulary gives 0 and 0.
+    workspace: a uint8 CUDA tensor of fp8q_policy_loss_workspace bytes (a new
+    one when None)."""
+    r = _fast().token_logprobs(logits, tokens, temperature, logp, entropy, workspace)
+    if r is not None:
+        return _done(r, "fp8q_token_logprobs")
+    dtype, T, V, workspace = _logits(logits, tokens, workspace)
+    logp = _new_vector(logp, torch.float32, T, "logp", logits.device)
+    entropy = _new_vector(entropy, torch.float32, T, "entropy", logits.device)
+    st = lib().fp8q_token_logprobs(logits.data_ptr(), dtype, T, V, _ld(logits), tokens.data_ptr(), float(temperature),
+                                   logp.data_ptr(), entropy.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                   _stream(logits))
+    _check(st, "fp8q_token_logprobs")
+    return logp, entropy
+
+
+def policy_loss(logits, tokens, logp_old, adv, weight, clip_low, clip_high, beta=0.0, logp_ref=None, w_tis=None,
+                temperature=1.0, clip=None, loss=None, dlogits=None, logp=None, entropy=None, workspace=None):
+    """The clipped policy loss with truncated importance sampling and a KL
+    term, and its gradient in the logits (see fp8q_policy_loss): returns
+    (loss [1], dlogits, logp, entropy).  tokens int64 [T]; logp_old, adv,
+    weight (0: the token does not count) and, optionally, logp_ref and w_tis
+    fp32 [T]; clip: the `result` tensor of calibrate_clip(), whose new bounds
+    then replace clip_low and clip_high without a copy to the host; `dlogits`
+    may be the logits."""
+    r = _fast().policy_loss(logits, tokens, logp_old, adv, weight, clip_low, clip_high, beta, logp_ref, w_tis,
+                            temperature, clip, loss, dlogits, logp, entropy, workspace)
+    if r is not None:
+        return _done(r, "fp8q_policy_loss")
+    dtype, T, V, workspace = _logits(logits, tokens, workspace)
+    dev = logits.device
+    batch = PolicyBatch(tokens=tokens.data_ptr(), clip_low=float(clip_low), clip_high=float(clip_high),
+                        beta=float(beta), temperature=float(temperature))
+    for name, t in (("logp_old", logp_old), ("adv", adv), ("weight", weight), ("w_tis", w_tis), ("logp_ref", logp_ref)):
+        if t is not None or name in ("logp_old", "adv", "weight"):
+            setattr(batch, name, _vector(t, torch.float32, T, name, dev).data_ptr())
+    if clip is not None:
+        batch.clip = _vector(clip, torch.uint8, ctypes.sizeof(ClipResult), "clip", dev).data_ptr()
+    loss = _new_vector(loss, torch.float32, 1, "loss", dev)
+    dlogits = _given(dlogits, logits.dtype, "dlogits", (T, V), dev)
+    logp = _new_vector(logp, torch.float32, T, "logp", dev)
+    entropy = _new_vector(entropy, torch.float32, T, "entropy", dev)
+    st = lib().fp8q_policy_loss(logits.data_ptr(), dtype, T, V, _ld(logits), ctypes.byref(batch), loss.data_ptr(),
+                                dlogits.data_ptr(), _ld(dlogits), logp.data_ptr(), entropy.data_ptr(),
+                                workspace.data_ptr(), workspace.numel(), _stream(logits))
+    _check(st, "fp8q_policy_loss")
+    return loss, dlogits, logp, entropy

@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libfp8q.so")
 NATIVE = os.path.join(PKG, "_native.so")
-SOURCES = ["abi.hip", "quantize.hip", "gemm.hip", "clip.hip"]
+SOURCES = ["abi.hip", "abi_ops.hip", "quantize.hip", "gemm.hip", "gated.hip", "clip.hip", "norm.hip", "requantize.hip", "loss.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -25,7 +25,7 @@ FLAGS = [
 # Per-source additions.  GEMM: matrix-instruction results in ordinary VGPRs
 # (the compiler otherwise puts the 128 x 128 and 64 x 64 tiles' partials in
 # AGPRs, and every promotion FMA then waits for a v_accvgpr_read copy).
-EXTRA = {"gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("gemm.hip", "gated.hip")}
 
 
 def check_no_scratch(src, remarks):

@@ -39,6 +39,17 @@ struct Api {
   decltype(&fp8q_gemm_splitk) gemm_splitk;
   decltype(&fp8q_calibrate_clip_workspace) clip_workspace;
   decltype(&fp8q_calibrate_clip) calibrate_clip;
+  decltype(&fp8q_rmsnorm) rmsnorm;
+  decltype(&fp8q_rmsnorm_quantize) rmsnorm_quantize;
+  decltype(&fp8q_rmsnorm_backward_workspace) norm_workspace;
+  decltype(&fp8q_rmsnorm_backward) rmsnorm_backward;
+  decltype(&fp8q_gemm_gated) gemm_gated;
+  decltype(&fp8q_gemm_gated_quantized) gemm_gated_quantized;
+  decltype(&fp8q_gated_backward) gated_backward;
+  decltype(&fp8q_requantize_transposed) requantize_transposed;
+  decltype(&fp8q_policy_loss_workspace) loss_workspace;
+  decltype(&fp8q_token_logprobs) token_logprobs;
+  decltype(&fp8q_policy_loss) policy_loss;
 };
 constexpr Py_ssize_t kApiSize = sizeof(Api) / sizeof(void*);
 
@@ -387,6 +398,312 @@ PyObject* py_calibrate_clip(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The norm's weight, [cols] in bf16 or fp32, and its flag.
+const void* norm_weight(PyObject* o, int64_t cols, c10::Device device, unsigned& flag) {
+  const at::Tensor& w = tensor(o);
+  flag = w.scalar_type() == at::kFloat ? FP8Q_WEIGHT_F32 : 0u;
+  if (w.dim() != 1 || w.size(0) != cols) leave();
+  return vector(o, flag ? at::kFloat : at::kBFloat16, cols, device).const_data_ptr();
+}
+
+// What both norms are given but for their output, and h and rstd.
+struct Norm {
+  const void *x, *residual = nullptr, *weight;
+  int64_t rows, cols, ldx, ldr = 0, ldh = 0;
+  unsigned flag;
+  void* h = nullptr;
+  float* rstd;
+  at::Tensor ht, rt;
+  PyObject* given_h;
+  c10::Device device;
+  ihipStream_t* stream;
+  Norm(PyObject* ox, PyObject* ow, PyObject* ores, PyObject* oh, PyObject* orstd) : device(tensor(ox).device()) {
+    const at::Tensor& t = matrix(ox, at::kBFloat16);
+    x = t.const_data_ptr();
+    rows = t.size(0);
+    cols = t.size(1);
+    ldx = t.stride(0);
+    stream = stream_of(t);
+    weight = norm_weight(ow, cols, device, flag);
+    rt = vector_or_new(orstd, at::kFloat, rows, device);
+    rstd = rt.mutable_data_ptr<float>();
+    given_h = oh;
+    if (ores == Py_None) {
+      if (oh != Py_None) leave();
+      given_h = ox;  // h is x itself
+      return;
+    }
+    const at::Tensor& r = matrix(ores, at::kBFloat16);
+    if (r.size(0) != rows || r.size(1) != cols || r.device() != device) leave();
+    residual = r.const_data_ptr();
+    ldr = r.stride(0);
+    ht = matrix_or_new(oh, at::kBFloat16, rows, cols, device);
+    h = ht.mutable_data_ptr();
+    ldh = ht.stride(0);
+  }
+};
+
+// rmsnorm(x, weight, eps, residual, out, h, rstd) -> (out, h, rstd)
+PyObject* py_rmsnorm(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<7>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const Norm p(a[0], a[1], a[3], a[5], a[6]);
+    const float eps = (float)real(a[2]);
+    const at::Tensor y = matrix_or_new(a[4], at::kBFloat16, p.rows, p.cols, p.device);
+    void* yp = y.mutable_data_ptr();
+    const fp8q_status st = unlocked([&] {
+      return api.rmsnorm(p.x, p.ldx, p.residual, p.ldr, p.weight, p.flag, p.rows, p.cols, eps, p.h, p.ldh, p.rstd, yp,
+                         y.stride(0), p.stream);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[4], y), give(p.given_h, p.ht), give(a[6], p.rt)});
+  });
+}
+
+// rmsnorm_quantize(x, weight, eps, granularity, flags, residual, codes,
+// scales, h, rstd) -> (codes, scales, h, rstd)
+PyObject* py_rmsnorm_quantize(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<10>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const Norm p(a[0], a[1], a[5], a[8], a[9]);
+    const float eps = (float)real(a[2]);
+    const auto g = (fp8q_granularity)integer(a[3]);
+    const unsigned flags = (unsigned)integer(a[4]) | p.flag;
+    const int64_t ns = api.scales_count(p.rows, p.cols, g, 0);
+    if (ns < 0) leave();
+    const at::Tensor codes = matrix_or_new(a[6], at::kByte, p.rows, p.cols, p.device);
+    const at::Tensor scales = vector_or_new(a[7], at::kFloat, ns, p.device);
+    uint8_t* cp = codes.mutable_data_ptr<uint8_t>();
+    float* sp = scales.mutable_data_ptr<float>();
+    const fp8q_status st = unlocked([&] {
+      return api.rmsnorm_quantize(p.x, p.ldx, p.residual, p.ldr, p.weight, flags, p.rows, p.cols, eps, p.h, p.ldh,
+                                  p.rstd, g, cp, codes.stride(0), sp, p.stream);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[6], codes), give(a[7], scales), give(p.given_h, p.ht), give(a[9], p.rt)});
+  });
+}
+
+// rmsnorm_backward(dy, h, rstd, weight, dres, dx, dweight, workspace) -> (dx,
+// dweight)
+PyObject* py_rmsnorm_backward(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<8>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const at::Tensor &dy = matrix(a[0], at::kBFloat16), &h = matrix(a[1], at::kBFloat16);
+    const int64_t rows = dy.size(0), cols = dy.size(1);
+    const c10::Device device = dy.device();
+    if (h.size(0) != rows || h.size(1) != cols || h.device() != device) leave();
+    const float* rstd = vector(a[2], at::kFloat, rows, device).const_data_ptr<float>();
+    unsigned flag;
+    const void* w = norm_weight(a[3], cols, device, flag);
+    const void* dres = nullptr;
+    int64_t ldres = 0;
+    if (a[4] != Py_None) {
+      const at::Tensor& r = matrix(a[4], at::kBFloat16);
+      if (r.size(0) != rows || r.size(1) != cols || r.device() != device) leave();
+      dres = r.const_data_ptr();
+      ldres = r.stride(0);
+    }
+    const int64_t need = api.norm_workspace(rows, cols);
+    if (need < 0) leave();
+    const at::Tensor dx = matrix_or_new(a[5], at::kBFloat16, rows, cols, device);
+    const at::Tensor dw = vector_or_new(a[6], at::kFloat, cols, device);
+    const at::Tensor ws = vector_or_new(a[7], at::kByte, need, device);
+    const void *dyp = dy.const_data_ptr(), *hp = h.const_data_ptr();
+    void *dxp = dx.mutable_data_ptr(), *wp = ws.mutable_data_ptr();
+    float* dwp = dw.mutable_data_ptr<float>();
+    const int64_t bytes = ws.numel();
+    ihipStream_t* s = stream_of(dy);
+    const fp8q_status st = unlocked([&] {
+      return api.rmsnorm_backward(dyp, dy.stride(0), hp, h.stride(0), rstd, w, flag, dres, ldres, rows, cols, dxp,
+                                  dx.stride(0), dwp, wp, bytes, s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[5], dx), give(a[6], dw)});
+  });
+}
+
+bool truth(PyObject* o) {
+  if (o != Py_True && o != Py_False) leave();
+  return o == Py_True;
+}
+
+// gemm_gated(a, sa, b, sb, save, out, pre) -> (out, pre) and
+// gemm_gated_quantized(a, sa, b, sb, save, codes, scales, pre) -> (codes,
+// scales, pre)
+template <bool QOUT>
+PyObject* py_gemm_gated(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<QOUT ? 8 : 7>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const Operands p = operands(api, a[0], a[1], FP8Q_BLOCK_1x128, a[2], a[3], FP8Q_BLOCK_128x128);
+    PyObject* const given_pre = a[QOUT ? 7 : 6];
+    if (p.N % 2) leave();
+    const int64_t F = p.N / 2;
+    at::Tensor pre;
+    void* pp = nullptr;
+    int64_t ldp = 0;
+    if (truth(a[4]) || given_pre != Py_None) {
+      pre = matrix_or_new(given_pre, at::kBFloat16, p.M, p.N, p.device);
+      pp = pre.mutable_data_ptr();
+      ldp = pre.stride(0);
+    }
+    auto kept = [&]() -> PyObject* {
+      if (pp) return give(given_pre, pre);
+      Py_RETURN_NONE;
+    };
+    if (QOUT) {
+      const int64_t ns = api.scales_count(p.M, F, FP8Q_BLOCK_1x128, 0);
+      if (ns < 0) leave();
+      const at::Tensor codes = matrix_or_new(a[5], at::kByte, p.M, F, p.device);
+      const at::Tensor scales = vector_or_new(a[6], at::kFloat, ns, p.device);
+      uint8_t* cp = codes.mutable_data_ptr<uint8_t>();
+      float* sp = scales.mutable_data_ptr<float>();
+      const fp8q_status st = unlocked([&] {
+        return api.gemm_gated_quantized(p.a, p.sa, p.lda, p.b, p.sb, p.ldb, p.M, F, p.K, pp, ldp, cp, codes.stride(0),
+                                        sp, p.stream);
+      });
+      if (st != FP8Q_OK) return PyLong_FromLong(st);
+      return pack({give(a[5], codes), give(a[6], scales), kept()});
+    }
+    const at::Tensor out = matrix_or_new(a[5], at::kBFloat16, p.M, F, p.device);
+    void* op = out.mutable_data_ptr();
+    const fp8q_status st = unlocked([&] {
+      return api.gemm_gated(p.a, p.sa, p.lda, p.b, p.sb, p.ldb, p.M, F, p.K, op, out.stride(0), pp, ldp, p.stream);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[5], out), kept()});
+  });
+}
+
+// gated_backward(dh, pre, flags, codes_r, scales_r, codes_t, scales_t) -> the
+// four
+PyObject* py_gated_backward(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<7>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const at::Tensor &dh = matrix(a[0], at::kBFloat16), &pre = matrix(a[1], at::kBFloat16);
+    const unsigned flags = (unsigned)integer(a[2]);
+    const int64_t M = dh.size(0), F = dh.size(1), Mp = (M + 127) / 128 * 128;
+    const c10::Device device = dh.device();
+    if (pre.size(0) != M || pre.size(1) != 2 * F || pre.device() != device) leave();
+    const at::Tensor cr = matrix_or_new(a[3], at::kByte, M, 2 * F, device);
+    const at::Tensor sr = vector_or_new(a[4], at::kFloat, M * (2 * F / 128), device);
+    const at::Tensor ct = matrix_or_new(a[5], at::kByte, 2 * F, Mp, device);
+    const at::Tensor sct = vector_or_new(a[6], at::kFloat, Mp / 128 * 2 * F, device);
+    const void *dhp = dh.const_data_ptr(), *pp = pre.const_data_ptr();
+    uint8_t *crp = cr.mutable_data_ptr<uint8_t>(), *ctp = ct.mutable_data_ptr<uint8_t>();
+    float *srp = sr.mutable_data_ptr<float>(), *stp = sct.mutable_data_ptr<float>();
+    ihipStream_t* s = stream_of(dh);
+    const fp8q_status st = unlocked([&] {
+      return api.gated_backward(dhp, dh.stride(0), pp, pre.stride(0), M, F, flags, crp, cr.stride(0), srp, ctp,
+                                ct.stride(0), stp, s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[3], cr), give(a[4], sr), give(a[5], ct), give(a[6], sct)});
+  });
+}
+
+// requantize_transposed(codes, scales, flags, codes_t, scales_t) -> (codes_t,
+// scales_t)
+PyObject* py_requantize_transposed(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<5>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const at::Tensor& codes = matrix(a[0], at::kByte);
+    const unsigned flags = (unsigned)integer(a[2]);
+    const int64_t rows = codes.size(0), cols = codes.size(1), Rp = (rows + 127) / 128 * 128;
+    const c10::Device device = codes.device();
+    const int64_t ns = api.scales_count(rows, cols, FP8Q_BLOCK_1x128, 0);
+    if (ns < 0) leave();
+    const float* sp = vector(a[1], at::kFloat, ns, device).const_data_ptr<float>();
+    const at::Tensor ct = matrix_or_new(a[3], at::kByte, cols, Rp, device);
+    const at::Tensor sct = vector_or_new(a[4], at::kFloat, Rp / 128 * cols, device);
+    const uint8_t* cp = codes.const_data_ptr<uint8_t>();
+    uint8_t* ctp = ct.mutable_data_ptr<uint8_t>();
+    float* stp = sct.mutable_data_ptr<float>();
+    ihipStream_t* s = stream_of(codes);
+    const fp8q_status st = unlocked([&] {
+      return api.requantize_transposed(cp, codes.stride(0), sp, rows, cols, flags, ctp, ct.stride(0), stp, s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[3], ct), give(a[4], sct)});
+  });
+}
+
+// Logits, tokens and workspace of the two calls on them.
+struct Logits {
+  const void* x;
+  fp8q_dtype dtype;
+  int64_t T, V, ld, bytes;
+  const int64_t* tokens;
+  at::Tensor ws;
+  void* wp;
+  c10::Device device;
+  ihipStream_t* stream;
+  Logits(const Api& api, PyObject* ox, PyObject* ot, PyObject* ow) : device(tensor(ox).device()) {
+    dtype = tensor(ox).scalar_type() == at::kFloat ? FP8Q_F32 : FP8Q_BF16;
+    const at::Tensor& t = matrix(ox, type());
+    x = t.const_data_ptr();
+    T = t.size(0);
+    V = t.size(1);
+    ld = t.stride(0);
+    tokens = vector(ot, at::kLong, T, device).const_data_ptr<int64_t>();
+    const int64_t need = api.loss_workspace(T, V);
+    if (need < 0) leave();
+    ws = vector_or_new(ow, at::kByte, need, device);
+    wp = ws.mutable_data_ptr();
+    bytes = ws.numel();
+    stream = stream_of(t);
+  }
+  at::ScalarType type() const { return dtype == FP8Q_F32 ? at::kFloat : at::kBFloat16; }
+};
+
+// token_logprobs(logits, tokens, temperature, logp, entropy, workspace) ->
+// (logp, entropy)
+PyObject* py_token_logprobs(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<6>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const Logits p(api, a[0], a[1], a[5]);
+    const double temperature = real(a[2]);
+    const at::Tensor logp = vector_or_new(a[3], at::kFloat, p.T, p.device);
+    const at::Tensor entropy = vector_or_new(a[4], at::kFloat, p.T, p.device);
+    float *lp = logp.mutable_data_ptr<float>(), *ep = entropy.mutable_data_ptr<float>();
+    const fp8q_status st = unlocked([&] {
+      return api.token_logprobs(p.x, p.dtype, p.T, p.V, p.ld, p.tokens, temperature, lp, ep, p.wp, p.bytes, p.stream);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[3], logp), give(a[4], entropy)});
+  });
+}
+
+// policy_loss(logits, tokens, logp_old, adv, weight, clip_low, clip_high,
+// beta, logp_ref, w_tis, temperature, clip, loss, dlogits, logp, entropy,
+// workspace) -> (loss, dlogits, logp, entropy)
+PyObject* py_policy_loss(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<17>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const Logits p(api, a[0], a[1], a[16]);
+    auto tokenwise = [&](PyObject* o) { return vector(o, at::kFloat, p.T, p.device).const_data_ptr<float>(); };
+    fp8q_policy_batch b{};
+    b.tokens = p.tokens;
+    b.logp_old = tokenwise(a[2]);
+    b.adv = tokenwise(a[3]);
+    b.weight = tokenwise(a[4]);
+    if (a[8] != Py_None) b.logp_ref = tokenwise(a[8]);
+    if (a[9] != Py_None) b.w_tis = tokenwise(a[9]);
+    b.clip_low = real(a[5]);
+    b.clip_high = real(a[6]);
+    b.beta = real(a[7]);
+    b.temperature = real(a[10]);
+    if (a[11] != Py_None)
+      b.clip = static_cast<const fp8q_clip_result*>(
+          vector(a[11], at::kByte, sizeof(fp8q_clip_result), p.device).const_data_ptr());
+    const at::Tensor loss = vector_or_new(a[12], at::kFloat, 1, p.device);
+    const at::Tensor dlogits = matrix_or_new(a[13], p.type(), p.T, p.V, p.device);
+    const at::Tensor logp = vector_or_new(a[14], at::kFloat, p.T, p.device);
+    const at::Tensor entropy = vector_or_new(a[15], at::kFloat, p.T, p.device);
+    float *lossp = loss.mutable_data_ptr<float>(), *lp = logp.mutable_data_ptr<float>();
+    float* ep = entropy.mutable_data_ptr<float>();
+    void* dp = dlogits.mutable_data_ptr();
+    const fp8q_status st = unlocked([&] {
+      return api.policy_loss(p.x, p.dtype, p.T, p.V, p.ld, &b, lossp, dp, dlogits.stride(0), lp, ep, p.wp, p.bytes,
+                             p.stream);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[12], loss), give(a[13], dlogits), give(a[14], logp), give(a[15], entropy)});
+  });
+}
+
 // bind((address, ..)): the entry points of Api, in its order
 PyObject* py_bind(PyObject* m, PyObject* addresses) {
   if (!PyTuple_CheckExact(addresses) || PyTuple_GET_SIZE(addresses) != kApiSize) {
@@ -416,6 +733,15 @@ PyMethodDef methods[] = {
     {"gemm_quantized", FAST(py_gemm_quantized), nullptr},
     {"gemm_grouped", FAST(py_gemm_grouped), nullptr},
     {"calibrate_clip", FAST(py_calibrate_clip), nullptr},
+    {"rmsnorm", FAST(py_rmsnorm), nullptr},
+    {"rmsnorm_quantize", FAST(py_rmsnorm_quantize), nullptr},
+    {"rmsnorm_backward", FAST(py_rmsnorm_backward), nullptr},
+    {"gemm_gated", FAST(py_gemm_gated<false>), nullptr},
+    {"gemm_gated_quantized", FAST(py_gemm_gated<true>), nullptr},
+    {"gated_backward", FAST(py_gated_backward), nullptr},
+    {"requantize_transposed", FAST(py_requantize_transposed), nullptr},
+    {"token_logprobs", FAST(py_token_logprobs), nullptr},
+    {"policy_loss", FAST(py_policy_loss), nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, sizeof(Api), methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,538 @@
+// Log-probabilities of the taken tokens, and the clipped policy loss with a KL
+// term, forward and backward, from the logits of each token on gfx950.
+//
+// With z = x / temperature over a row of V logits, and the taken token a,
+//   lse = log sum exp(z),  p = exp(z - lse),  logp = z_a - lse,
+//   entropy = lse - sum p z,
+//   r = exp(logp - logp_old),  d = logp_ref - logp,
+//   l = -w min(r A, clip(r, low, high) A) + beta (exp(d) - d - 1),
+//   l' = dl / dlogp = -w A r [r A <= clip(r) A] + beta (1 - exp(d)),
+//   loss = sum c l,  dx_j = c l' / temperature (delta_aj - p_j)
+// over the tokens with weight c != 0 and a inside the vocabulary; all other
+// rows are not read: their results and gradients are zero.
+//
+// Bound by HBM: the logits read once, the gradient written once.  So a
+// workgroup holds a whole row in registers between the two (131072 bf16 logits
+// are half of a CU's registers), takes the running maximum, sum and entropy sum
+// while its pieces arrive, and writes the gradient from the registers.  Longer
+// rows read what exceeds them again.  Too few rows to fill the chip are split
+// over several workgroups, which leave their sums in a workspace, and a second
+// kernel joins them.  Everything is in base 2 (one fused multiply-add and one
+// v_exp_f32 an element), with the temperature in the factor log2(e) / t.
+#include <type_traits>
+
+#include "device_common.h"
+#include "ops.h"
+
+namespace fp8q {
+
+namespace loss_detail {
+
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
+constexpr float kNegInf = -__builtin_inff();
+
+// A 16-byte piece of logits as fp32 and back.
+template <bool F32>
+struct Piece {
+  static constexpr int kN = F32 ? 4 : 8;
+  static constexpr int kSize = F32 ? 4 : 2;
+  static __device__ __forceinline__ void widen(const uint4& p, float (&v)[kN]) {
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (F32) {
+        v[e] = __uint_as_float(w[e]);
+      } else {
+        v[2 * e] = bf16_lo(w[e]);
+        v[2 * e + 1] = bf16_hi(w[e]);
+      }
+    }
+  }
+  static __device__ __forceinline__ uint4 narrow(const float (&v)[kN]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (F32)
+        w[e] = __float_as_uint(v[e]);
+      else
+        w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{v[2 * e], v[2 * e + 1]}), v2bf));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ uint4 nothing() {  // -inf throughout
+    const uint32_t w = F32 ? 0xff800000u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
+  }
+  static __device__ __forceinline__ float load(const uint8_t* row, int64_t i) {
+    if constexpr (F32) return reinterpret_cast<const float*>(row)[i];
+    return bf16_lo(reinterpret_cast<const uint16_t*>(row)[i]);
+  }
+  static __device__ __forceinline__ void store(uint8_t* row, int64_t i, float v) {
+    if constexpr (F32) {
+      reinterpret_cast<float*>(row)[i] = v;
+    } else {
+      reinterpret_cast<__bf16*>(row)[i] = (__bf16)v;
+    }
+  }
+};
+
+// Running sums of a softmax relative to 2^m: s = sum 2^(t - m), q = sum
+// 2^(t - m) (t - m), over t = x log2(e) / temperature; m = -inf: none yet.
+struct Sums {
+  float m, s, q;
+};
+
+// The sums of both; each side's are taken to the larger maximum.
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b) {
+  const float m = fmaxf(a.m, b.m);
+  // (a side without a finite logit has m = -inf and nothing to rescale; one
+  // with +inf or NaN carries NaN in s)
+  const float da = a.m == m ? 0.0f : a.m - m, db = b.m == m ? 0.0f : b.m - m;
+  const float fa = a.m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(da);
+  const float fb = b.m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(db);
+  Sums r;
+  r.m = m;
+  r.s = a.s * fa + b.s * fb;
+  r.q = fa * (a.m == kNegInf ? a.q : __builtin_fmaf(a.s, da, a.q)) +
+        fb * (b.m == kNegInf ? b.q : __builtin_fmaf(b.s, db, b.q));
+  return r;
+}
+
+// The sums of one element t = x log2(e) / temperature (s is 1, and NaN for +inf
+// or NaN).
+__device__ __forceinline__ Sums single(float t) { return Sums{t, t == kNegInf ? 0.0f : 1.0f + (t - t), 0.0f}; }
+
+__device__ __forceinline__ Sums shuffled(const Sums& a, int mask) {
+  return Sums{__shfl_xor(a.m, mask, 64), __shfl_xor(a.s, mask, 64), __shfl_xor(a.q, mask, 64)};
+}
+
+__device__ __forceinline__ Sums wave_join(Sums a) {
+#pragma unroll
+  for (int mask = 1; mask < 64; mask *= 2) a = join(a, shuffled(a, mask));
+  return a;
+}
+
+// Adds K pieces to a thread's sums.
+template <bool F32, int K>
+__device__ __forceinline__ void add_pieces(const uint4* p, float c, Sums& a) {
+  using P = Piece<F32>;
+  float top = kNegInf;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    float v[P::kN];
+    P::widen(p[k], v);
+#pragma unroll
+    for (int e = 0; e < P::kN; ++e) top = fmaxf(top, v[e]);
+  }
+  const float m = fmaxf(a.m, top * c);
+  const float ref = m == kNegInf ? 0.0f : m;
+  if (a.m != kNegInf) {
+    const float d = a.m - ref, f = __builtin_amdgcn_exp2f(d);
+    a.q = f * __builtin_fmaf(a.s, d, a.q);
+    a.s *= f;
+  }
+  a.m = m;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    float v[P::kN];
+    P::widen(p[k], v);
+#pragma unroll
+    for (int e = 0; e < P::kN; ++e) {
+      const float u = __builtin_fmaf(v[e], c, -ref);
+      const float x = __builtin_amdgcn_exp2f(u);
+      a.s += x;
+      a.q = __builtin_fmaf(x, fmaxf(u, -1e30f), a.q);  // (a logit of -inf adds 0, not 0 * -inf)
+    }
+  }
+}
+
+// A row of logits: `full` aligned 16-byte pieces from element `head` on, and
+// before and after them fewer than a piece's elements each, one a thread.
+template <bool F32>
+struct Row {
+  using P = Piece<F32>;
+  const uint8_t* base;
+  int64_t V, head, full;
+  __device__ __forceinline__ Row(const void* logits, int64_t ld, int64_t row, int64_t v) {
+    V = v;
+    base = static_cast<const uint8_t*>(logits) + row * ld * P::kSize;
+    const int64_t lead = (16 - (int64_t)((uintptr_t)base & 15)) % 16 / P::kSize;
+    head = lead < V ? lead : V;
+    full = (V - head) / P::kN;
+  }
+  __device__ __forceinline__ const uint4* piece(int64_t j) const {
+    return reinterpret_cast<const uint4*>(base + head * P::kSize) + j;
+  }
+  // this thread's single element: its index, or -1
+  __device__ __forceinline__ int64_t edge(int t) const {
+    if (t < head) return t;
+    const int64_t i = head + full * P::kN + (t - 32);
+    return t >= 32 && i < V ? i : -1;
+  }
+};
+
+// What the loss needs of a token besides its logits, and what its row gets.
+struct Token {
+  float k;  // c l' / temperature
+  float logp, entropy, term;
+};
+
+__device__ __forceinline__ Token token_of(const LossArgs& a, int64_t row, const Sums& sums, float x, bool grad) {
+  Token o{};
+  const float c = a.inv_temperature * kLog2e;
+  const float log_s = logf(sums.s);
+  // (x c - m) ln 2 - log s; entropy = log s - ln 2 q / s, both relative to 2^m
+  o.logp = __builtin_fmaf(__builtin_fmaf(x, c, sums.m == kNegInf ? -0.0f : -sums.m), kLn2, -log_s);
+  o.entropy = log_s - kLn2 * (sums.q / sums.s);
+  if (!grad) return o;
+  const float low = a.clip ? (float)a.clip->l_new : a.clip_low, high = a.clip ? (float)a.clip->h_new : a.clip_high;
+  const float adv = a.adv[row], w = a.w_tis ? a.w_tis[row] : 1.0f, weight = a.weight[row];
+  const float r = expf(o.logp - a.logp_old[row]);
+  const float plain = r * adv, cut = fminf(fmaxf(r, low), high) * adv;
+  float l = -w * (plain > cut ? cut : plain);
+  float slope = plain > cut ? 0.0f : -w * plain;
+  if (a.logp_ref) {
+    const float d = a.logp_ref[row] - o.logp, e = expm1f(d);
+    l += a.beta * (e - d);
+    slope -= a.beta * e;
+  }
+  o.term = weight * l;
+  o.k = weight * slope * a.inv_temperature;
+  return o;
+}
+
+// Whether the row counts: its token lies in the vocabulary and, for the loss,
+// its weight is not zero.
+__device__ __forceinline__ bool counts(const LossArgs& a, int64_t row, int64_t token, bool grad) {
+  return token >= 0 && token < a.V && (!grad || a.weight[row] != 0.0f);
+}
+
+// dx of a piece at vocabulary index i0: (delta - p) k, with p = 2^(x c - m) / s
+// and ks = k / s.
+template <bool F32>
+__device__ __forceinline__ uint4 piece_gradient(const uint4& p, float c, float ref, float k, float ks, int64_t i0,
+                                                int64_t token) {
+  using P = Piece<F32>;
+  float v[P::kN];
+  P::widen(p, v);
+#pragma unroll
+  for (int e = 0; e < P::kN; ++e) v[e] = -ks * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], c, -ref));
+  const int64_t at = token - i0;
+  if (at >= 0 && at < P::kN) {
+#pragma unroll
+    for (int e = 0; e < P::kN; ++e) v[e] += at == e ? k : 0.0f;
+  }
+  return P::narrow(v);
+}
+
+// Writes a piece of the gradient; `aligned`: the row of dlogits is aligned as
+// the row of logits.
+template <bool F32>
+__device__ __forceinline__ void store_piece(uint8_t* out, int64_t i0, bool aligned, const uint4& p) {
+  using P = Piece<F32>;
+  if (aligned) {
+    *reinterpret_cast<uint4*>(out + i0 * P::kSize) = p;
+  } else {
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+    for (int e = 0; e < P::kN; ++e) {
+      if constexpr (F32)
+        reinterpret_cast<uint32_t*>(out)[i0 + e] = w[e];
+      else
+        reinterpret_cast<uint16_t*>(out)[i0 + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+    }
+  }
+}
+
+// A row's gradient of zeros, by THREADS threads.
+template <bool F32, int THREADS>
+__device__ __forceinline__ void store_zeros(const LossArgs& a, int64_t row, int64_t first, int64_t last, int t) {
+  using P = Piece<F32>;
+  uint8_t* const out = static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize;
+  for (int64_t i = first + t; i < last; i += THREADS) P::store(out, i, 0.0f);
+}
+
+// One workgroup a row.  GRAD: the first NV pieces of every thread stay in
+// registers for the gradient; the others are read again.
+template <bool F32, int THREADS, int NV, bool GRAD>
+__global__ __launch_bounds__(THREADS) void row_kernel(LossArgs a) {
+  using P = Piece<F32>;
+  constexpr int W = THREADS / 64, kChunk = NV % 4 == 0 ? 4 : 1;
+  __shared__ Sums parts[W];
+  __shared__ Token shared;
+  const int t = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const int64_t token = a.tokens[row];
+  if (!counts(a, row, token, GRAD)) {  // the whole workgroup
+    if (GRAD) store_zeros<F32, THREADS>(a, row, 0, a.V, t);
+    if (t == 0) {
+      a.logp[row] = 0.0f;
+      a.entropy[row] = 0.0f;
+      if (GRAD) a.terms[row] = 0.0f;
+    }
+    return;
+  }
+  const float c = a.inv_temperature * kLog2e;
+  const Row<F32> x(a.logits, a.ld, row, a.V);
+  const float mine = P::load(x.base, token);
+  const int64_t edge = x.edge(t);
+  float ev = kNegInf;
+  if (edge >= 0) ev = P::load(x.base, edge);
+
+  uint4 held[NV];
+  Sums sums{kNegInf, 0.0f, 0.0f};
+  auto fetch = [&](int64_t j0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t j = j0 + (int64_t)i * THREADS + t;
+      held[i] = P::nothing();
+      if (j < x.full) held[i] = *x.piece(j);
+    }
+  };
+  auto add = [&]() {
+#pragma unroll
+    for (int i = 0; i < NV; i += kChunk) add_pieces<F32, kChunk>(held + i, c, sums);
+  };
+  // the pieces past the first NV of each thread, if any, then those
+  constexpr int64_t kStep = (int64_t)NV * THREADS;
+  for (int64_t j0 = (x.full + kStep - 1) / kStep * kStep - kStep; j0 >= kStep; j0 -= kStep) {
+    fetch(j0);
+    add();
+  }
+  fetch(0);
+  add();
+  if (edge >= 0) sums = join(sums, single(ev * c));
+  sums = wave_join(sums);
+  if ((t & 63) == 0) parts[t >> 6] = sums;
+  __syncthreads();
+  sums = parts[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) sums = join(sums, parts[w]);
+  if (t == 0) {
+    const Token o = token_of(a, row, sums, mine, GRAD);
+    a.logp[row] = o.logp;
+    a.entropy[row] = o.entropy;
+    if (GRAD) {
+      a.terms[row] = o.term;
+      shared = o;
+    }
+  }
+  if constexpr (GRAD) {
+    __syncthreads();
+    const float k = shared.k, ks = k / sums.s, ref = sums.m == kNegInf ? 0.0f : sums.m;
+    uint8_t* const out = static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize;
+    const bool aligned = (((uintptr_t)out ^ (uintptr_t)x.base) & 15) == 0;
+    auto put = [&](int64_t j0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int64_t j = j0 + (int64_t)i * THREADS + t, i0 = x.head + j * P::kN;
+        if (j < x.full) store_piece<F32>(out, i0, aligned, piece_gradient<F32>(held[i], c, ref, k, ks, i0, token));
+      }
+    };
+    put(0);
+    for (int64_t j0 = kStep; j0 < x.full; j0 += kStep) {
+      fetch(j0);
+      put(j0);
+    }
+    if (edge >= 0)
+      P::store(out, edge, (edge == token ? k : 0.0f) - ks * __builtin_amdgcn_exp2f(__builtin_fmaf(ev, c, -ref)));
+  }
+}
+
+// Few rows: workgroup (part, row) takes every piece j with j / per == part, and
+// part 0 the row's edges.
+constexpr int kSplitThreads = 256;
+
+template <bool F32, bool GRAD>
+__global__ __launch_bounds__(kSplitThreads) void split_sums_kernel(LossArgs a, int64_t per) {
+  using P = Piece<F32>;
+  constexpr int W = kSplitThreads / 64, NV = 8;
+  __shared__ Sums shared[W];
+  const int t = threadIdx.x;
+  const int64_t part = blockIdx.x, row = blockIdx.y;
+  if (!counts(a, row, a.tokens[row], GRAD)) return;
+  const float c = a.inv_temperature * kLog2e;
+  const Row<F32> x(a.logits, a.ld, row, a.V);
+  const int64_t first = part * per, last = first + per < x.full ? first + per : x.full;
+  Sums sums{kNegInf, 0.0f, 0.0f};
+  for (int64_t j0 = first; j0 < last; j0 += NV * kSplitThreads) {
+    uint4 held[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t j = j0 + (int64_t)i * kSplitThreads + t;
+      held[i] = P::nothing();
+      if (j < last) held[i] = *x.piece(j);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; i += 4) add_pieces<F32, 4>(held + i, c, sums);
+  }
+  const int64_t edge = part == 0 ? x.edge(t) : -1;
+  if (edge >= 0) sums = join(sums, single(P::load(x.base, edge) * c));
+  sums = wave_join(sums);
+  if ((t & 63) == 0) shared[t >> 6] = sums;
+  __syncthreads();
+  if (t == 0) {
+#pragma unroll
+    for (int w = 1; w < W; ++w) sums = join(sums, shared[w]);
+    float* const p = a.partials + (row * kLossParts + part) * 4;
+    p[0] = sums.m;
+    p[1] = sums.s;
+    p[2] = sums.q;
+    if (part == 0) p[3] = P::load(x.base, a.tokens[row]);  // (dlogits may be written over the logits)
+  }
+}
+
+// A row's sums from its parts, joined in one order by every wave that asks.
+__device__ __forceinline__ Sums joined(const LossArgs& a, int64_t row, int parts) {
+  const int lane = threadIdx.x & 63;
+  Sums s{kNegInf, 0.0f, 0.0f};
+  if (lane < parts) {
+    const float* const p = a.partials + (row * kLossParts + lane) * 4;
+    s = Sums{p[0], p[1], p[2]};
+  }
+  return wave_join(s);
+}
+
+// The log-probabilities of split rows: a wave a row.
+__global__ __launch_bounds__(64) void split_logprobs_kernel(LossArgs a, int parts) {
+  const int64_t row = blockIdx.x;
+  Token o{};
+  if (counts(a, row, a.tokens[row], false))
+    o = token_of(a, row, joined(a, row, parts), a.partials[row * kLossParts * 4 + 3], false);
+  if (threadIdx.x == 0) {
+    a.logp[row] = o.logp;
+    a.entropy[row] = o.entropy;
+  }
+}
+
+template <bool F32>
+__global__ __launch_bounds__(kSplitThreads) void split_gradient_kernel(LossArgs a, int64_t per, int parts) {
+  using P = Piece<F32>;
+  constexpr int NV = 4;
+  const int t = threadIdx.x;
+  const int64_t part = blockIdx.x, row = blockIdx.y;
+  const int64_t token = a.tokens[row];
+  const Row<F32> x(a.logits, a.ld, row, a.V);
+  const int64_t first = part * per, last = first + per < x.full ? first + per : x.full;
+  const int64_t edge = part == 0 ? x.edge(t) : -1;
+  if (!counts(a, row, token, true)) {
+    store_zeros<F32, kSplitThreads>(a, row, x.head + first * P::kN, x.head + last * P::kN, t);
+    if (edge >= 0) P::store(static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize, edge, 0.0f);
+    if (part == 0 && t == 0) a.logp[row] = a.entropy[row] = a.terms[row] = 0.0f;
+    return;
+  }
+  const float c = a.inv_temperature * kLog2e;
+  const Sums sums = joined(a, row, parts);
+  const Token o = token_of(a, row, sums, a.partials[row * kLossParts * 4 + 3], true);
+  if (part == 0 && t == 0) {
+    a.logp[row] = o.logp;
+    a.entropy[row] = o.entropy;
+    a.terms[row] = o.term;
+  }
+  const float ks = o.k / sums.s, ref = sums.m == kNegInf ? 0.0f : sums.m;
+  uint8_t* const out = static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize;
+  const bool aligned = (((uintptr_t)out ^ (uintptr_t)x.base) & 15) == 0;
+  for (int64_t j0 = first; j0 < last; j0 += NV * kSplitThreads) {
+    uint4 held[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t j = j0 + (int64_t)i * kSplitThreads + t;
+      held[i] = P::nothing();
+      if (j < last) held[i] = *x.piece(j);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t j = j0 + (int64_t)i * kSplitThreads + t, i0 = x.head + j * P::kN;
+      if (j < last) store_piece<F32>(out, i0, aligned, piece_gradient<F32>(held[i], c, ref, o.k, ks, i0, token));
+    }
+  }
+  if (edge >= 0) {
+    const float ev = P::load(x.base, edge);
+    P::store(out, edge, (edge == token ? o.k : 0.0f) - ks * __builtin_amdgcn_exp2f(__builtin_fmaf(ev, c, -ref)));
+  }
+}
+
+// The loss from the tokens' parts, in float64, in a fixed order.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(const float* terms, int64_t T, float* loss) {
+  __shared__ double lds[kSumThreads];
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < T; i += kSumThreads) s += (double)terms[i];
+  lds[threadIdx.x] = s;
+  __syncthreads();
+  for (int n = kSumThreads / 2; n > 0; n /= 2) {
+    if ((int)threadIdx.x < n) lds[threadIdx.x] += lds[threadIdx.x + n];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *loss = (float)lds[0];
+}
+
+// Pieces of each of the workgroups that share a row, and their number.
+inline int split_parts(int64_t T, int64_t pieces, int64_t& per) {
+  int64_t parts = (1024 + T - 1) / T;
+  const int64_t most = (pieces + kSplitThreads * 4 - 1) / (kSplitThreads * 4);  // of four pieces a thread or more
+  if (parts > most) parts = most;
+  if (parts > kLossParts) parts = kLossParts;
+  if (parts < 1) parts = 1;
+  per = (pieces + parts - 1) / parts;
+  return (int)parts;
+}
+
+template <bool F32, bool GRAD>
+hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
+  constexpr int N = Piece<F32>::kN;
+  const int64_t pieces = a.V / N + 1;
+  if (a.T < kLossSplitRows && pieces > 2 * kSplitThreads) {
+    int64_t per;
+    const int parts = split_parts(a.T, pieces, per);
+    const dim3 grid((unsigned)parts, (unsigned)a.T);
+    split_sums_kernel<F32, GRAD><<<grid, kSplitThreads, 0, s>>>(a, per);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (GRAD)
+      split_gradient_kernel<F32><<<grid, kSplitThreads, 0, s>>>(a, per, parts);
+    else
+      split_logprobs_kernel<<<dim3((unsigned)a.T), 64, 0, s>>>(a, parts);
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)a.T);
+  if (!GRAD) {
+    if (pieces <= 4 * 256)
+      row_kernel<F32, 256, 4, GRAD><<<grid, 256, 0, s>>>(a);
+    else
+      row_kernel<F32, 512, 8, GRAD><<<grid, 512, 0, s>>>(a);
+  } else if (pieces <= 4 * 256) {
+    row_kernel<F32, 256, 4, GRAD><<<grid, 256, 0, s>>>(a);
+  } else if (pieces <= 8 * 256) {
+    row_kernel<F32, 256, 8, GRAD><<<grid, 256, 0, s>>>(a);
+  } else if (pieces <= 16 * 256) {
+    row_kernel<F32, 256, 16, GRAD><<<grid, 256, 0, s>>>(a);
+  } else if (pieces <= 16 * 512) {
+    row_kernel<F32, 512, 16, GRAD><<<grid, 512, 0, s>>>(a);
+  } else if (pieces <= 16 * 1024) {
+    row_kernel<F32, 1024, 16, GRAD><<<grid, 1024, 0, s>>>(a);
+  } else {
+    row_kernel<F32, 1024, 20, GRAD><<<grid, 1024, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace loss_detail
+
+using namespace loss_detail;
+
+hipError_t launch_logprobs(const LossArgs& a, hipStream_t s) {
+  return a.f32 ? launch_rows<true, false>(a, s) : launch_rows<false, false>(a, s);
+}
+
+hipError_t launch_policy_loss(const LossArgs& a, hipStream_t s) {
+  const hipError_t e = a.f32 ? launch_rows<true, true>(a, s) : launch_rows<false, true>(a, s);
+  if (e != hipSuccess) return e;
+  loss_sum_kernel<<<1, kSumThreads, 0, s>>>(a.terms, a.T, a.loss);
+  return hipGetLastError();
+}
+
+}  // namespace fp8q
