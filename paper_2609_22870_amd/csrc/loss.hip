@@ -79,6 +79,10 @@ struct Piece {
   }
 };
 
+// From here on p is another value to the compiler: it would else keep the fp32
+// form of every held piece from the sums to the gradient, and spill.
+__device__ __forceinline__ void forget(uint4& p) { asm volatile("" : "+v"(p.x), "+v"(p.y), "+v"(p.z), "+v"(p.w)); }
+
 // Running sums of a softmax relative to 2^m: s = sum 2^(t - m), q = sum
 // 2^(t - m) (t - m), over t = x log2(e) / temperature; m = -inf: none yet.
 struct Sums {
@@ -109,9 +113,11 @@ __device__ __forceinline__ Sums shuffled(const Sums& a, int mask) {
   return Sums{__shfl_xor(a.m, mask, 64), __shfl_xor(a.s, mask, 64), __shfl_xor(a.q, mask, 64)};
 }
 
+// The sums of N neighbouring lanes (every lane gets the same bits).
+template <int N = 64>
 __device__ __forceinline__ Sums wave_join(Sums a) {
 #pragma unroll
-  for (int mask = 1; mask < 64; mask *= 2) a = join(a, shuffled(a, mask));
+  for (int mask = 1; mask < N; mask *= 2) a = join(a, shuffled(a, mask));
   return a;
 }
 
@@ -151,26 +157,33 @@ __device__ __forceinline__ void add_pieces(const uint4* p, float c, Sums& a) {
 
 // A row of logits: `full` aligned 16-byte pieces from element `head` on, and
 // before and after them fewer than a piece's elements each, one a thread.
+// Everything but the thread's own part of an address is the same in the whole
+// workgroup, so a piece's address is a scalar and one 32-bit offset for all
+// pieces (64-bit ones for each took the registers that hold the row).
 template <bool F32>
 struct Row {
   using P = Piece<F32>;
   const uint8_t* base;
-  int64_t V, head, full;
+  int V, head, full;
   __device__ __forceinline__ Row(const void* logits, int64_t ld, int64_t row, int64_t v) {
-    V = v;
+    V = (int)v;
     base = static_cast<const uint8_t*>(logits) + row * ld * P::kSize;
-    const int64_t lead = (16 - (int64_t)((uintptr_t)base & 15)) % 16 / P::kSize;
+    const int lead = (16 - (int)((uintptr_t)base & 15)) % 16 / P::kSize;
     head = lead < V ? lead : V;
     full = (V - head) / P::kN;
   }
-  __device__ __forceinline__ const uint4* piece(int64_t j) const {
-    return reinterpret_cast<const uint4*>(base + head * P::kSize) + j;
+  // piece j0 + t, where that is below last
+  __device__ __forceinline__ uint4 piece(int j0, int last, unsigned t) const {
+    uint4 p = P::nothing();
+    if ((int)t < last - j0)
+      p = *reinterpret_cast<const uint4*>(base + head * P::kSize + (int64_t)j0 * 16 + t * 16u);
+    return p;
   }
   // this thread's single element: its index, or -1
-  __device__ __forceinline__ int64_t edge(int t) const {
+  __device__ __forceinline__ int edge(int t) const {
     if (t < head) return t;
-    const int64_t i = head + full * P::kN + (t - 32);
-    return t >= 32 && i < V ? i : -1;
+    const int i = head + full * P::kN + (t - 32);
+    return t >= 32 && t < 32 + P::kN && i < V ? i : -1;
   }
 };
 
@@ -210,42 +223,56 @@ __device__ __forceinline__ bool counts(const LossArgs& a, int64_t row, int64_t t
   return token >= 0 && token < a.V && (!grad || a.weight[row] != 0.0f);
 }
 
-// dx of a piece at vocabulary index i0: (delta - p) k, with p = 2^(x c - m) / s
-// and ks = k / s.
+// A row's gradient: dx_j = (delta - p) k, p = 2^(x c - m) / s, ks = k / s.
 template <bool F32>
-__device__ __forceinline__ uint4 piece_gradient(const uint4& p, float c, float ref, float k, float ks, int64_t i0,
-                                                int64_t token) {
+struct Gradient {
   using P = Piece<F32>;
-  float v[P::kN];
-  P::widen(p, v);
-#pragma unroll
-  for (int e = 0; e < P::kN; ++e) v[e] = -ks * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], c, -ref));
-  const int64_t at = token - i0;
-  if (at >= 0 && at < P::kN) {
-#pragma unroll
-    for (int e = 0; e < P::kN; ++e) v[e] += at == e ? k : 0.0f;
+  uint8_t* out;
+  bool aligned;  // as the row of logits is, so that pieces go out whole
+  int head, token;
+  float c, ref, k, ks;
+  __device__ __forceinline__ Gradient(const LossArgs& a, int64_t row, const Row<F32>& x, int64_t tok, const Sums& sums,
+                                      float kk) {
+    out = static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize;
+    aligned = (((uintptr_t)out ^ (uintptr_t)x.base) & 15) == 0;
+    head = x.head;
+    token = (int)tok;
+    c = a.inv_temperature * kLog2e;
+    ref = sums.m == kNegInf ? 0.0f : sums.m;
+    k = kk;
+    ks = kk / sums.s;
   }
-  return P::narrow(v);
-}
-
-// Writes a piece of the gradient; `aligned`: the row of dlogits is aligned as
-// the row of logits.
-template <bool F32>
-__device__ __forceinline__ void store_piece(uint8_t* out, int64_t i0, bool aligned, const uint4& p) {
-  using P = Piece<F32>;
-  if (aligned) {
-    *reinterpret_cast<uint4*>(out + i0 * P::kSize) = p;
-  } else {
-    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+  __device__ __forceinline__ float of(float x, bool taken) const {
+    return (taken ? k : 0.0f) - ks * __builtin_amdgcn_exp2f(__builtin_fmaf(x, c, -ref));
+  }
+  // of piece j0 + t, where that is below last
+  __device__ __forceinline__ void put(const uint4& p, int j0, int last, unsigned t) const {
+    if ((int)t >= last - j0) return;
+    float v[P::kN];
+    P::widen(p, v);
 #pragma unroll
-    for (int e = 0; e < P::kN; ++e) {
-      if constexpr (F32)
-        reinterpret_cast<uint32_t*>(out)[i0 + e] = w[e];
-      else
-        reinterpret_cast<uint16_t*>(out)[i0 + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+    for (int e = 0; e < P::kN; ++e) v[e] = -ks * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], c, -ref));
+    const unsigned at = (unsigned)(token - head - j0 * P::kN) - t * P::kN;
+    if (at < (unsigned)P::kN) {
+#pragma unroll
+      for (int e = 0; e < P::kN; ++e) v[e] += at == (unsigned)e ? k : 0.0f;
+    }
+    const uint4 g = P::narrow(v);
+    uint8_t* const to = out + head * P::kSize + (int64_t)j0 * 16;
+    if (aligned) {
+      *reinterpret_cast<uint4*>(to + t * 16u) = g;
+    } else {
+      const uint32_t w[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+      for (int e = 0; e < P::kN; ++e) {
+        if constexpr (F32)
+          reinterpret_cast<uint32_t*>(to)[t * 4u + e] = w[e];
+        else
+          reinterpret_cast<uint16_t*>(to)[t * 8u + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+      }
     }
   }
-}
+};
 
 // A row's gradient of zeros, by THREADS threads.
 template <bool F32, int THREADS>
@@ -278,27 +305,26 @@ __global__ __launch_bounds__(THREADS) void row_kernel(LossArgs a) {
   const float c = a.inv_temperature * kLog2e;
   const Row<F32> x(a.logits, a.ld, row, a.V);
   const float mine = P::load(x.base, token);
-  const int64_t edge = x.edge(t);
+  const int edge = x.edge(t);
   float ev = kNegInf;
   if (edge >= 0) ev = P::load(x.base, edge);
 
   uint4 held[NV];
   Sums sums{kNegInf, 0.0f, 0.0f};
-  auto fetch = [&](int64_t j0) {
+  auto fetch = [&](int j0) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t j = j0 + (int64_t)i * THREADS + t;
-      held[i] = P::nothing();
-      if (j < x.full) held[i] = *x.piece(j);
-    }
+    for (int i = 0; i < NV; ++i) held[i] = x.piece(j0 + i * THREADS, x.full, t);
   };
   auto add = [&]() {
 #pragma unroll
-    for (int i = 0; i < NV; i += kChunk) add_pieces<F32, kChunk>(held + i, c, sums);
+    for (int i = 0; i < NV; i += kChunk) {
+      add_pieces<F32, kChunk>(held + i, c, sums);
+      __builtin_amdgcn_sched_barrier(0);  // one chunk's fp32 values live at a time
+    }
   };
   // the pieces past the first NV of each thread, if any, then those
-  constexpr int64_t kStep = (int64_t)NV * THREADS;
-  for (int64_t j0 = (x.full + kStep - 1) / kStep * kStep - kStep; j0 >= kStep; j0 -= kStep) {
+  constexpr int kStep = NV * THREADS;
+  for (int j0 = kStep; j0 < x.full; j0 += kStep) {
     fetch(j0);
     add();
   }
@@ -308,9 +334,7 @@ __global__ __launch_bounds__(THREADS) void row_kernel(LossArgs a) {
   sums = wave_join(sums);
   if ((t & 63) == 0) parts[t >> 6] = sums;
   __syncthreads();
-  sums = parts[0];
-#pragma unroll
-  for (int w = 1; w < W; ++w) sums = join(sums, parts[w]);
+  sums = wave_join<W>(parts[t & (W - 1)]);
   if (t == 0) {
     const Token o = token_of(a, row, sums, mine, GRAD);
     a.logp[row] = o.logp;
@@ -322,23 +346,21 @@ __global__ __launch_bounds__(THREADS) void row_kernel(LossArgs a) {
   }
   if constexpr (GRAD) {
     __syncthreads();
-    const float k = shared.k, ks = k / sums.s, ref = sums.m == kNegInf ? 0.0f : sums.m;
-    uint8_t* const out = static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize;
-    const bool aligned = (((uintptr_t)out ^ (uintptr_t)x.base) & 15) == 0;
-    auto put = [&](int64_t j0) {
+    const Gradient<F32> g(a, row, x, token, sums, shared.k);
+    auto put = [&](int j0) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int64_t j = j0 + (int64_t)i * THREADS + t, i0 = x.head + j * P::kN;
-        if (j < x.full) store_piece<F32>(out, i0, aligned, piece_gradient<F32>(held[i], c, ref, k, ks, i0, token));
+        forget(held[i]);
+        g.put(held[i], j0 + i * THREADS, x.full, t);
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
     put(0);
-    for (int64_t j0 = kStep; j0 < x.full; j0 += kStep) {
+    for (int j0 = kStep; j0 < x.full; j0 += kStep) {
       fetch(j0);
       put(j0);
     }
-    if (edge >= 0)
-      P::store(out, edge, (edge == token ? k : 0.0f) - ks * __builtin_amdgcn_exp2f(__builtin_fmaf(ev, c, -ref)));
+    if (edge >= 0) P::store(g.out, edge, g.of(ev, edge == g.token));
   }
 }
 
@@ -347,7 +369,7 @@ __global__ __launch_bounds__(THREADS) void row_kernel(LossArgs a) {
 constexpr int kSplitThreads = 256;
 
 template <bool F32, bool GRAD>
-__global__ __launch_bounds__(kSplitThreads) void split_sums_kernel(LossArgs a, int64_t per) {
+__global__ __launch_bounds__(kSplitThreads) void split_sums_kernel(LossArgs a, int per) {
   using P = Piece<F32>;
   constexpr int W = kSplitThreads / 64, NV = 8;
   __shared__ Sums shared[W];
@@ -356,20 +378,16 @@ __global__ __launch_bounds__(kSplitThreads) void split_sums_kernel(LossArgs a, i
   if (!counts(a, row, a.tokens[row], GRAD)) return;
   const float c = a.inv_temperature * kLog2e;
   const Row<F32> x(a.logits, a.ld, row, a.V);
-  const int64_t first = part * per, last = first + per < x.full ? first + per : x.full;
+  const int first = (int)part * per, last = first + per < x.full ? first + per : x.full;
   Sums sums{kNegInf, 0.0f, 0.0f};
-  for (int64_t j0 = first; j0 < last; j0 += NV * kSplitThreads) {
+  for (int j0 = first; j0 < last; j0 += NV * kSplitThreads) {
     uint4 held[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t j = j0 + (int64_t)i * kSplitThreads + t;
-      held[i] = P::nothing();
-      if (j < last) held[i] = *x.piece(j);
-    }
+    for (int i = 0; i < NV; ++i) held[i] = x.piece(j0 + i * kSplitThreads, last, t);
 #pragma unroll
     for (int i = 0; i < NV; i += 4) add_pieces<F32, 4>(held + i, c, sums);
   }
-  const int64_t edge = part == 0 ? x.edge(t) : -1;
+  const int edge = part == 0 ? x.edge(t) : -1;
   if (edge >= 0) sums = join(sums, single(P::load(x.base, edge) * c));
   sums = wave_join(sums);
   if ((t & 63) == 0) shared[t >> 6] = sums;
@@ -409,22 +427,21 @@ __global__ __launch_bounds__(64) void split_logprobs_kernel(LossArgs a, int part
 }
 
 template <bool F32>
-__global__ __launch_bounds__(kSplitThreads) void split_gradient_kernel(LossArgs a, int64_t per, int parts) {
+__global__ __launch_bounds__(kSplitThreads) void split_gradient_kernel(LossArgs a, int per, int parts) {
   using P = Piece<F32>;
   constexpr int NV = 4;
   const int t = threadIdx.x;
   const int64_t part = blockIdx.x, row = blockIdx.y;
   const int64_t token = a.tokens[row];
   const Row<F32> x(a.logits, a.ld, row, a.V);
-  const int64_t first = part * per, last = first + per < x.full ? first + per : x.full;
-  const int64_t edge = part == 0 ? x.edge(t) : -1;
+  const int first = (int)part * per, last = first + per < x.full ? first + per : x.full;
+  const int edge = part == 0 ? x.edge(t) : -1;
   if (!counts(a, row, token, true)) {
     store_zeros<F32, kSplitThreads>(a, row, x.head + first * P::kN, x.head + last * P::kN, t);
     if (edge >= 0) P::store(static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize, edge, 0.0f);
     if (part == 0 && t == 0) a.logp[row] = a.entropy[row] = a.terms[row] = 0.0f;
     return;
   }
-  const float c = a.inv_temperature * kLog2e;
   const Sums sums = joined(a, row, parts);
   const Token o = token_of(a, row, sums, a.partials[row * kLossParts * 4 + 3], true);
   if (part == 0 && t == 0) {
@@ -432,27 +449,15 @@ __global__ __launch_bounds__(kSplitThreads) void split_gradient_kernel(LossArgs 
     a.entropy[row] = o.entropy;
     a.terms[row] = o.term;
   }
-  const float ks = o.k / sums.s, ref = sums.m == kNegInf ? 0.0f : sums.m;
-  uint8_t* const out = static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize;
-  const bool aligned = (((uintptr_t)out ^ (uintptr_t)x.base) & 15) == 0;
-  for (int64_t j0 = first; j0 < last; j0 += NV * kSplitThreads) {
+  const Gradient<F32> g(a, row, x, token, sums, o.k);
+  for (int j0 = first; j0 < last; j0 += NV * kSplitThreads) {
     uint4 held[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t j = j0 + (int64_t)i * kSplitThreads + t;
-      held[i] = P::nothing();
-      if (j < last) held[i] = *x.piece(j);
-    }
+    for (int i = 0; i < NV; ++i) held[i] = x.piece(j0 + i * kSplitThreads, last, t);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t j = j0 + (int64_t)i * kSplitThreads + t, i0 = x.head + j * P::kN;
-      if (j < last) store_piece<F32>(out, i0, aligned, piece_gradient<F32>(held[i], c, ref, o.k, ks, i0, token));
-    }
+    for (int i = 0; i < NV; ++i) g.put(held[i], j0 + i * kSplitThreads, last, t);
   }
-  if (edge >= 0) {
-    const float ev = P::load(x.base, edge);
-    P::store(out, edge, (edge == token ? o.k : 0.0f) - ks * __builtin_amdgcn_exp2f(__builtin_fmaf(ev, c, -ref)));
-  }
+  if (edge >= 0) P::store(g.out, edge, g.of(P::load(x.base, edge), edge == g.token));
 }
 
 // The loss from the tokens' parts, in float64, in a fixed order.
@@ -471,13 +476,13 @@ __global__ __launch_bounds__(kSumThreads) void loss_sum_kernel(const float* term
 }
 
 // Pieces of each of the workgroups that share a row, and their number.
-inline int split_parts(int64_t T, int64_t pieces, int64_t& per) {
+inline int split_parts(int64_t T, int64_t pieces, int& per) {
   int64_t parts = (1024 + T - 1) / T;
   const int64_t most = (pieces + kSplitThreads * 4 - 1) / (kSplitThreads * 4);  // of four pieces a thread or more
   if (parts > most) parts = most;
   if (parts > kLossParts) parts = kLossParts;
   if (parts < 1) parts = 1;
-  per = (pieces + parts - 1) / parts;
+  per = (int)((pieces + parts - 1) / parts);
   return (int)parts;
 }
 
@@ -486,7 +491,7 @@ hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
   constexpr int N = Piece<F32>::kN;
   const int64_t pieces = a.V / N + 1;
   if (a.T < kLossSplitRows && pieces > 2 * kSplitThreads) {
-    int64_t per;
+    int per;
     const int parts = split_parts(a.T, pieces, per);
     const dim3 grid((unsigned)parts, (unsigned)a.T);
     split_sums_kernel<F32, GRAD><<<grid, kSplitThreads, 0, s>>>(a, per);
@@ -515,7 +520,7 @@ hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
   } else if (pieces <= 16 * 1024) {
     row_kernel<F32, 1024, 16, GRAD><<<grid, 1024, 0, s>>>(a);
   } else {
-    row_kernel<F32, 1024, 20, GRAD><<<grid, 1024, 0, s>>>(a);
+    row_kernel<F32, 1024, F32 ? 18 : 20, GRAD><<<grid, 1024, 0, s>>>(a);
   }
   return hipGetLastError();
 }
