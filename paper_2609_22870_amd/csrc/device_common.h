@@ -67,6 +67,28 @@ __device__ __forceinline__ UnitScale unit_scale_fmt(float amax, bool pow2) {
   return pow2 ? unit_scale_pow2(amax, E5 ? 16 : 9) : unit_scale(amax, fp8_max<E5>());
 }
 
+// The same scale without IEEE divisions, for kernels whose every lane forms its
+// units' own: with r = RN(1 / F_max), q = RN(a r) and the exact residual e = a -
+// q F_max, RN(q + e r) is RN32(a / F_max) for every a in the normal range (checked
+// for every mantissa on the CPU); 1 / S is a reciprocal with one Newton step, good
+// to an ulp, which the quotient's own residual step corrects.  Units with a smaller
+// amax (zero among them) take the divisions.
+__device__ __noinline__ inline UnitScale small_unit_scale(float amax, float fmax) { return unit_scale(amax, fmax); }
+
+template <bool E5>
+__device__ __forceinline__ UnitScale quick_unit_scale(float amax, bool pow2) {
+  if (pow2) return unit_scale_pow2(amax, E5 ? 16 : 9);
+  constexpr float kMax = fp8_max<E5>(), kInv = 1.0f / kMax;
+  UnitScale u;
+  const float q = amax * kInv;
+  u.s = __builtin_fmaf(__builtin_fmaf(-q, kMax, amax), kInv, q);
+  const float r = __builtin_amdgcn_rcpf(u.s);
+  u.r = __builtin_fmaf(__builtin_fmaf(-u.s, r, 1.0f), r, r);
+  u.fast = true;
+  if (amax < 0x1p-64f) u = small_unit_scale(amax, kMax);
+  return u;
+}
+
 // RN32(x / S) for a bf16 x of the unit whose scale is u.  For S >= 2^-90 the
 // quotient is formed from the reciprocal with one residual correction,
 //   q0 = RN(x r),  e = RN(q0 S - x) (one FMA),  q = RN(q0 - e r) (one FMA);

@@ -165,7 +165,7 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e] * rstd * w[i][e]));
     }
-    u = unit_scale(row_reduce<THREADS, true>(m, lds + W), a.pow2 != 0);
+    u = quick_unit_scale<false>(row_reduce<THREADS, true>(m, lds + W), a.pow2 != 0);
     if (t == 0) a.scales[r] = u.s;
   }
 #pragma unroll
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
       float m = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
-      u = unit_scale(row16_max(m), a.pow2 != 0);
+      u = quick_unit_scale<false>(row16_max(m), a.pow2 != 0);
       if ((t & 15) == 0 && c < a.cols) a.scales[(c >> 7) * a.rows + r] = u.s;
     }
     if (c < a.cols) {

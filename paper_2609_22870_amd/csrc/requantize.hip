@@ -1,22 +1,144 @@
-// Activations kept in 8 bits for the backward pass, on gfx950: the codes that a
-// forward GEMM took (1x128 units along the features) become the weight-gradient
-// GEMM's operand (Eq. 3 in units of 128 tokens, transposed),
-//   v = RN32(S code),  S' = RN32(amax over 128 rows of |v| / 448),
-//   codes'[c][r] = E4M3 of v / S',
-// without the activation ever being held in 16 bits.  A last unit of fewer than
-// 128 rows is filled up with zeros, so that the GEMM's contraction stays a whole
-// number of units.
+// Operands of the backward GEMMs that are made from what the forward pass kept,
+// on gfx950: a weight gradient's from an activation's 8-bit codes, and the two
+// of a gated activation's gradient.
 //
-// Bound by HBM: one byte read and one written an element, and 4 / 128 twice for
-// the scales.
+// A workgroup takes a tile of 128 x 128 elements, 8 rows x COLS columns a thread
+// in fp32 registers.  The 128 / COLS lanes of a tile row share its 1x128 unit;
+// the rows' groups meet in LDS for the 128x1 units' maxima.  Every lane forms the
+// scales it needs itself (quick_unit_scale: ten instructions, less than the
+// shuffles or LDS exchanges and barriers of handing them round).  Codes that leave
+// transposed are packed along the rows, so that a thread's conversions already
+// give eight tokens of one column, and go through LDS only to leave in 16-byte
+// pieces.
+#include "device_common.h"
 #include "ops.h"
-#include "quant_tile.h"
 
 namespace fp8q {
 
-namespace quant_detail {
+namespace requant_detail {
+
+constexpr int kTile = 128;
 
 typedef float v2f __attribute__((ext_vector_type(2)));
+
+template <int COLS>
+struct Patch {
+  float v[8][COLS];
+};
+
+// Threads of a tile, lanes of a tile row, and groups of eight rows of a wave.
+template <int COLS>
+struct Shape {
+  static constexpr int kLanes = kTile / COLS, kThreads = kLanes * kTile / 8, kWaves = kThreads / 64;
+  static constexpr int kGroups = 64 / kLanes;
+};
+
+// Out of line: units with S < 2^-90 only.
+__device__ __noinline__ float slow_quotient(float x, float s) { return x / s; }
+
+__device__ __forceinline__ float code_quotient(float x, const UnitScale& u) {
+  return u.fast ? fast_quotient(x, u.s, u.r) : slow_quotient(x, u.s);
+}
+
+// Two codes into the low or high half of `old`, as fp8_pack2 without the clamp:
+// |x / S| is at most F_max (1 + 2^-23), which the conversion rounds to F_max.
+template <bool E5, bool HI>
+__device__ __forceinline__ uint32_t pack2(float a, float b, uint32_t old) {
+  return E5 ? (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(a, b, (int)old, HI)
+            : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)old, HI);
+}
+
+// Maximum over the lanes of a tile row.
+template <int COLS>
+__device__ __forceinline__ float row_max(float v) {
+  v = row16_max(v);
+  if constexpr (Shape<COLS>::kLanes > 16) v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return v;
+}
+
+// The patch's 1x128 codes to rows row0 .. row0 + 7 (those below `rows`) from
+// column c on, and their scales, [cols / 128][rows] at block c / 128.
+template <int COLS, bool E5>
+__device__ __forceinline__ void store_rows(const Patch<COLS>& p, bool pow2, int64_t row0, int64_t rows, int64_t c,
+                                           uint8_t* codes, int64_t ldc, float* scales) {
+  const int cc = threadIdx.x % Shape<COLS>::kLanes;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float m = 0.0f;
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) m = fmaxf(m, fabsf(p.v[i][j]));
+    const UnitScale u = quick_unit_scale<E5>(row_max<COLS>(m), pow2);
+    uint32_t w[COLS / 4];
+#pragma unroll
+    for (int j = 0; j < COLS; j += 4)
+      w[j / 4] = pack2<E5, true>(code_quotient(p.v[i][j + 2], u), code_quotient(p.v[i][j + 3], u),
+                                 pack2<E5, false>(code_quotient(p.v[i][j], u), code_quotient(p.v[i][j + 1], u), 0u));
+    const int64_t r = row0 + i;
+    if (r < rows) {
+      uint8_t* const to = codes + r * ldc + c;
+      if constexpr (COLS == 8)
+        *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+      else
+        *reinterpret_cast<uint32_t*>(to) = w[0];
+      if (cc == 0) scales[(c >> 7) * rows + r] = u.s;
+    }
+  }
+}
+
+// Column maxima of the wave's rows, to lds[wave][128].
+template <int COLS>
+__device__ __forceinline__ void leave_col_max(const Patch<COLS>& p, float (*lds)[kTile]) {
+  constexpr int L = Shape<COLS>::kLanes;
+  const int cc = threadIdx.x % L, lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < COLS; ++j) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(p.v[i][j]));
+    if constexpr (L == 16) m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    if (lane < L) lds[threadIdx.x >> 6][cc * COLS + j] = m;
+  }
+}
+
+// The patch's 128x1 codes, transposed, to LDS: line j of the tile (128 bytes, a
+// column's 128 tokens) holds in its eight-byte chunk g ^ (j / COLS % 16) the
+// tokens of row group g.  Then the scales, at scales + the tile's first column.
+template <int COLS, bool E5>
+__device__ __forceinline__ void leave_columns(const Patch<COLS>& p, bool pow2, const float (*lds)[kTile],
+                                              uint64_t* lines, float* scales) {
+  constexpr int L = Shape<COLS>::kLanes, W = Shape<COLS>::kWaves;
+  const int cc = threadIdx.x % L, rg = threadIdx.x / L;
+#pragma unroll
+  for (int j = 0; j < COLS; ++j) {
+    float m = lds[0][cc * COLS + j];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, lds[w][cc * COLS + j]);
+    const UnitScale u = quick_unit_scale<E5>(m, pow2);
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      w[h] = pack2<E5, true>(
+          code_quotient(p.v[4 * h + 2][j], u), code_quotient(p.v[4 * h + 3][j], u),
+          pack2<E5, false>(code_quotient(p.v[4 * h][j], u), code_quotient(p.v[4 * h + 1][j], u), 0u));
+    lines[(cc * COLS + j) * 16 + (rg ^ (cc & 15))] = (uint64_t)w[0] | ((uint64_t)w[1] << 32);
+    if (rg == 0) scales[cc * COLS + j] = u.s;
+  }
+}
+
+// The tile's lines from LDS to codes_t[c0 + j][r0 ..], in 16-byte pieces.
+template <int COLS>
+__device__ __forceinline__ void store_lines(const uint64_t* lines, uint8_t* codes_t, int64_t ldt, int64_t c0,
+                                            int64_t r0) {
+  constexpr int T = Shape<COLS>::kThreads;
+#pragma unroll
+  for (int x = threadIdx.x; x < kTile * 8; x += T) {
+    const int j = x >> 3, q = x & 7, sw = (j / COLS) & 15;
+    const uint64_t a = lines[j * 16 + ((2 * q) ^ sw)], b = lines[j * 16 + ((2 * q + 1) ^ sw)];
+    *reinterpret_cast<uint4*>(codes_t + (c0 + j) * ldt + r0 + q * 16) =
+        make_uint4((uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32));
+  }
+}
 
 // Two of the four codes in w (the low or the high 16 bits), as fp32.
 template <bool HI>
@@ -24,53 +146,49 @@ __device__ __forceinline__ v2f e4m3_values(uint32_t w) {
   return __builtin_amdgcn_cvt_pk_f32_fp8((int)w, HI);
 }
 
-__global__ __launch_bounds__(kThreads) void requant_kernel(RequantArgs a, int64_t padded_rows) {
-  __shared__ float lds_red[4 * kTile];
-  __shared__ uint64_t lds_t[kTile * kTile / 8];
-  const int cc = threadIdx.x & 15, rg = threadIdx.x >> 4;
-  const int64_t tr = blockIdx.y;
-  const int64_t r0 = tr * kTile, c0 = (int64_t)blockIdx.x * kTile;
-  const int64_t row0 = r0 + rg * 8, c = c0 + cc * 8;
+// Activations kept in 8 bits: the codes that a forward GEMM took (1x128 units
+// along the features) become the weight-gradient GEMM's operand (Eq. 3 in units
+// of 128 tokens, transposed),
+//   v = RN32(S code),  S' = RN32(amax over 128 rows of |v| / 448),
+//   codes'[c][r] = E4M3 of v / S',
+// without the activation ever being held in 16 bits.  A last unit of fewer than
+// 128 rows is filled up with zeros, so that the GEMM's contraction stays a whole
+// number of units.  Bound by HBM: one byte read and one written an element, and
+// 4 / 128 twice for the scales.
+constexpr int kRequantCols = 8;
 
+__global__ __launch_bounds__(Shape<kRequantCols>::kThreads) void requant_kernel(RequantArgs a) {
+  constexpr int C = kRequantCols, L = Shape<C>::kLanes;
+  __shared__ float lds[Shape<C>::kWaves][kTile];
+  __shared__ uint64_t lines[kTile * kTile / 8];
+  const int cc = threadIdx.x % L, rg = threadIdx.x / L;
+  const int64_t tr = blockIdx.y, r0 = tr * kTile, c0 = (int64_t)blockIdx.x * kTile;
+  const int64_t row0 = r0 + rg * 8, c = c0 + cc * C;
   uint2 w[8];
-  float sx[8];
+  float s[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t r = row0 + i;
     w[i] = make_uint2(0u, 0u);
-    sx[i] = 0.0f;
+    s[i] = 0.0f;
     if (r < a.rows) {
       w[i] = *reinterpret_cast<const uint2*>(a.codes + r * a.ldc + c);
-      sx[i] = a.scales[(int64_t)blockIdx.x * a.rows + r];
+      s[i] = a.scales[(int64_t)blockIdx.x * a.rows + r];
     }
   }
-  Tile t;
+  Patch<C> p;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const v2f v0 = e4m3_values<false>(w[i].x), v1 = e4m3_values<true>(w[i].x);
-    const v2f v2 = e4m3_values<false>(w[i].y), v3 = e4m3_values<true>(w[i].y);
-    t.v[i][0] = v0[0] * sx[i];
-    t.v[i][1] = v0[1] * sx[i];
-    t.v[i][2] = v1[0] * sx[i];
-    t.v[i][3] = v1[1] * sx[i];
-    t.v[i][4] = v2[0] * sx[i];
-    t.v[i][5] = v2[1] * sx[i];
-    t.v[i][6] = v3[0] * sx[i];
-    t.v[i][7] = v3[1] * sx[i];
-  }
-
-  UnitScale mine;
-  float m[8], su[8], ru[8];
-  tile_col_max(t, lds_red, m);
-  float amax = m[0];
+    const v2f v[4] = {e4m3_values<false>(w[i].x), e4m3_values<true>(w[i].x), e4m3_values<false>(w[i].y),
+                      e4m3_values<true>(w[i].y)};
 #pragma unroll
-  for (int j = 1; j < 8; ++j) amax = (rg & 7) == j ? m[j] : amax;
-  share_col_units<false>(amax, a.pow2 != 0, lds_red, mine, su, ru);
-  uint32_t packed[8][2];
-  encode_patch<kUnitCol, false>(t, su, ru, packed);
-  store_patch_transposed(packed, lds_t, a.codes_t, a.ldt, padded_rows, a.cols, r0, c0);
-  const int64_t cj = c0 + cc * 8 + rg;
-  if (rg < 8) a.scales_t[tr * a.cols + cj] = mine.s;
+    for (int j = 0; j < C; ++j) p.v[i][j] = v[j >> 1][j & 1] * s[i];
+  }
+  leave_col_max<C>(p, lds);
+  __syncthreads();
+  leave_columns<C, false>(p, a.pow2 != 0, lds, lines, a.scales_t + tr * a.cols + c0);
+  __syncthreads();
+  store_lines<C>(lines, a.codes_t, a.ldt, c0, r0);
 }
 
 // Gradients of a gated activation H = silu(G) U, from dH and the kept G and U:
@@ -79,8 +197,9 @@ __global__ __launch_bounds__(kThreads) void requant_kernel(RequantArgs a, int64_
 // both layouts of the backward GEMMs: codes per 1x128 unit for the data
 // gradient's, and transposed codes per 128x1 unit (the rows filled up to a
 // multiple of 128 with zeros) for the weight gradient's.  6 bytes read and 4
-// written for each element of H; a workgroup holds the 128 x 128 tiles of dG
-// and dU at one place in registers.
+// written for each element of H.  A workgroup holds the tiles of dG and dU at
+// one place: 8 x 4 patches, so that both fit the registers of four waves per
+// SIMD.
 __device__ __forceinline__ float sigmoid(float g) {
   // exp(-g) from exp2 with the product -g log2(e) in two parts, so that the
   // result keeps fp32 accuracy at any g; past +-88 (where s is 1 or below the
@@ -93,82 +212,71 @@ __device__ __forceinline__ float sigmoid(float g) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo * kLn2, e));
 }
 
-// The patch's codes in both layouts.
-template <bool E5>
-__device__ __forceinline__ void store_dual(const Tile& t, const GatedBackwardArgs& a, float* lds_red, uint64_t* lds_t,
-                                           int64_t padded_rows, int64_t tr, int64_t c0) {
-  const int cc = threadIdx.x & 15, rg = threadIdx.x >> 4;
-  const int64_t r0 = tr * kTile, row0 = r0 + rg * 8, c = c0 + cc * 8, cols = 2 * a.F;
-  UnitScale mine;
-  float su[8], ru[8];
-  uint32_t packed[8][2];
-  share_row_units<E5>(block_row_amax(t), a.pow2 != 0, mine, su, ru);
-  encode_patch<kUnitRow, E5>(t, su, ru, packed);
-  store_patch(packed, a.codes_r, a.ldr, a.M, cols, row0, c);
-  const int64_t r = row0 + cc;
-  if (cc < 8 && r < a.M) a.scales_r[(c >> 7) * a.M + r] = mine.s;
-  float m[8];
-  tile_col_max(t, lds_red, m);
-  float amax = m[0];
-#pragma unroll
-  for (int j = 1; j < 8; ++j) amax = (rg & 7) == j ? m[j] : amax;
-  share_col_units<E5>(amax, a.pow2 != 0, lds_red, mine, su, ru);
-  encode_patch<kUnitCol, E5>(t, su, ru, packed);
-  store_patch_transposed(packed, lds_t, a.codes_t, a.ldt, padded_rows, cols, r0, c0);
-  if (rg < 8) a.scales_t[tr * cols + c0 + cc * 8 + rg] = mine.s;
-}
+constexpr int kGatedCols = 4;
 
 template <bool E5>
-__global__ __launch_bounds__(kThreads) void gated_backward_kernel(GatedBackwardArgs a, int64_t padded_rows) {
-  __shared__ float lds_red[4 * kTile];
-  __shared__ uint64_t lds_t[kTile * kTile / 8];
-  const int cc = threadIdx.x & 15, rg = threadIdx.x >> 4;
-  const int64_t tr = blockIdx.y, c0 = (int64_t)blockIdx.x * kTile;
-  const int64_t row0 = tr * kTile + rg * 8, c = c0 + cc * 8;
-  Tile dg, du;
+__global__ __launch_bounds__(Shape<kGatedCols>::kThreads) void gated_backward_kernel(GatedBackwardArgs a) {
+  constexpr int C = kGatedCols, L = Shape<C>::kLanes;
+  __shared__ float lds[2][Shape<C>::kWaves][kTile];
+  __shared__ uint64_t lines[2][kTile * kTile / 8];
+  const int cc = threadIdx.x % L, rg = threadIdx.x / L;
+  const int64_t tr = blockIdx.y, r0 = tr * kTile, c0 = (int64_t)blockIdx.x * kTile;
+  const int64_t row0 = r0 + rg * 8, c = c0 + cc * C;
+  uint2 g[8], u[8], d[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t r = row0 + i;
-    uint4 g = make_uint4(0u, 0u, 0u, 0u), u = g, d = g;
+    g[i] = u[i] = d[i] = make_uint2(0u, 0u);
     if (r < a.M) {
-      g = *reinterpret_cast<const uint4*>(a.pre + r * a.ldp + c);
-      u = *reinterpret_cast<const uint4*>(a.pre + r * a.ldp + a.F + c);
-      d = *reinterpret_cast<const uint4*>(a.dh + r * a.lddh + c);
+      g[i] = *reinterpret_cast<const uint2*>(a.pre + r * a.ldp + c);
+      u[i] = *reinterpret_cast<const uint2*>(a.pre + r * a.ldp + a.F + c);
+      d[i] = *reinterpret_cast<const uint2*>(a.dh + r * a.lddh + c);
     }
-    const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, uw[4] = {u.x, u.y, u.z, u.w}, dw[4] = {d.x, d.y, d.z, d.w};
+  }
+  Patch<C> dg, du;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t gw[2] = {g[i].x, g[i].y}, uw[2] = {u[i].x, u[i].y}, dw[2] = {d[i].x, d[i].y};
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
       const float gv = j & 1 ? bf16_hi(gw[j >> 1]) : bf16_lo(gw[j >> 1]);
       const float uv = j & 1 ? bf16_hi(uw[j >> 1]) : bf16_lo(uw[j >> 1]);
       const float dv = j & 1 ? bf16_hi(dw[j >> 1]) : bf16_lo(dw[j >> 1]);
-      const float s = sigmoid(gv);
-      dg.v[i][j] = dv * uv * s * __builtin_fmaf(gv, 1.0f - s, 1.0f);
-      du.v[i][j] = dv * gv * s;
+      const float sig = sigmoid(gv), ds = dv * sig, dgs = ds * gv;
+      dg.v[i][j] = uv * __builtin_fmaf(dgs, 1.0f - sig, ds);
+      du.v[i][j] = dgs;
     }
   }
-  store_dual<E5>(dg, a, lds_red, lds_t, padded_rows, tr, c0);
-  __syncthreads();  // the tile's LDS is read before the next one's writes
-  store_dual<E5>(du, a, lds_red, lds_t, padded_rows, tr, a.F + c0);
+  const bool pow2 = a.pow2 != 0;
+  leave_col_max<C>(dg, lds[0]);
+  leave_col_max<C>(du, lds[1]);
+  store_rows<C, E5>(dg, pow2, row0, a.M, c, a.codes_r, a.ldr, a.scales_r);
+  store_rows<C, E5>(du, pow2, row0, a.M, a.F + c, a.codes_r, a.ldr, a.scales_r);
+  __syncthreads();
+  float* const st = a.scales_t + tr * 2 * a.F + c0;
+  leave_columns<C, E5>(dg, pow2, lds[0], lines[0], st);
+  leave_columns<C, E5>(du, pow2, lds[1], lines[1], st + a.F);
+  __syncthreads();
+  store_lines<C>(lines[0], a.codes_t, a.ldt, c0, r0);
+  store_lines<C>(lines[1], a.codes_t, a.ldt, a.F + c0, r0);
 }
 
-}  // namespace quant_detail
+}  // namespace requant_detail
 
-using namespace quant_detail;
+using namespace requant_detail;
 
 hipError_t launch_requantize_transposed(const RequantArgs& a, hipStream_t s) {
-  const int64_t tiles_r = (a.rows + kTile - 1) / kTile;
-  const dim3 grid((unsigned)(a.cols / kTile), (unsigned)tiles_r);
-  requant_kernel<<<grid, kThreads, 0, s>>>(a, tiles_r * kTile);
+  const dim3 grid((unsigned)(a.cols / kTile), (unsigned)((a.rows + kTile - 1) / kTile));
+  requant_kernel<<<grid, Shape<kRequantCols>::kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_gated_backward(const GatedBackwardArgs& a, hipStream_t s) {
-  const int64_t tiles_r = (a.M + kTile - 1) / kTile;
-  const dim3 grid((unsigned)(a.F / kTile), (unsigned)tiles_r);
+  const dim3 grid((unsigned)(a.F / kTile), (unsigned)((a.M + kTile - 1) / kTile));
   if (a.e5m2)
-    gated_backward_kernel<true><<<grid, kThreads, 0, s>>>(a, tiles_r * kTile);
+    gated_backward_kernel<true><<<grid, Shape<kGatedCols>::kThreads, 0, s>>>(a);
   else
-    gated_backward_kernel<false><<<grid, kThreads, 0, s>>>(a, tiles_r * kTile);
+    gated_backward_kernel<false><<<grid, Shape<kGatedCols>::kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
