@@ -495,9 +495,13 @@ fp8q_status fp8q_rmsnorm_backward(const void *dy, int64_t lddy, const void *h,
  * fp8q_gemm_gated_quantized writes H in 8 bits, for the down projection:
  * exactly fp8q_quantize(H, M, F, F, FP8Q_BLOCK_1x128, 0, codes, ldq, scales) of
  * the H that fp8q_gemm_gated computes; codes E4M3 [M][ldq], scales
- * [F/128][M].
+ * [F/128][M].  Sizes too small to give every CU a tile with whole units form H in
+ * a workspace first: device memory of at least fp8q_gemm_gated_workspace(M, F, K)
+ * bytes (0 for the others, whose workspace may be null), 16-byte aligned,
+ * overwritten.
  * Shape rules: K % 128 == 0, F % 128 == 0; 2 F ldb below 2^31, M K / 128 below
- * 2^29 and at most 2^22 tiles of 128 x 64 outputs (else FP8Q_ERR_UNSUPPORTED).  Alignment: A, B and codes 16-byte aligned, lda, ldb
+ * 2^29, M <= 65535 x 128, at most 2^22 tiles of 128 x 64 outputs, and 256 rows of
+ * A below 2^31 bytes where all of them are not (else FP8Q_ERR_UNSUPPORTED).  Alignment: A, B and codes 16-byte aligned, lda, ldb
  * and ldq multiples of 16; H and pre 8-byte aligned with ldh and ldp multiples
  * of 4; scales 4-byte aligned.  The outputs must not overlap each other or an
  * input.
@@ -507,12 +511,16 @@ fp8q_status fp8q_gemm_gated(const uint8_t *A, const float *sA, int64_t lda,
                             int64_t M, int64_t F, int64_t K, void *H,
                             int64_t ldh, void *pre, int64_t ldp,
                             struct ihipStream_t *stream);
+/* Bytes of workspace of fp8q_gemm_gated_quantized; -1 for a size <= 0 or above
+ * 2^31 - 1. */
+int64_t fp8q_gemm_gated_workspace(int64_t M, int64_t F, int64_t K);
 fp8q_status fp8q_gemm_gated_quantized(const uint8_t *A, const float *sA,
                                       int64_t lda, const uint8_t *B,
                                       const float *sB, int64_t ldb, int64_t M,
                                       int64_t F, int64_t K, void *pre,
                                       int64_t ldp, uint8_t *codes, int64_t ldq,
-                                      float *scales,
+                                      float *scales, void *workspace,
+                                      int64_t workspace_bytes,
                                       struct ihipStream_t *stream);
 
 /*

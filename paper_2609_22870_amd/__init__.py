@@ -37,7 +37,8 @@ EXPORTS = ("fp8q_scales_count", "fp8q_quantize", "fp8q_quantize_dual",
            "fp8q_calibrate_clip_workspace", "fp8q_calibrate_clip", "fp8q_calibrate_clip_noalloc",
            "fp8q_cast_f32",
            "fp8q_cast_f32_e5m2", "fp8q_rmsnorm", "fp8q_rmsnorm_quantize", "fp8q_rmsnorm_backward_workspace",
-           "fp8q_rmsnorm_backward", "fp8q_gemm_gated", "fp8q_gemm_gated_quantized", "fp8q_gated_backward",
+           "fp8q_rmsnorm_backward", "fp8q_gemm_gated", "fp8q_gemm_gated_workspace", "fp8q_gemm_gated_quantized",
+           "fp8q_gated_backward",
            "fp8q_requantize_transposed", "fp8q_policy_loss_workspace", "fp8q_token_logprobs", "fp8q_policy_loss",
            "fp8q_status_string")
 
@@ -95,7 +96,8 @@ _NATIVE_API = ("fp8q_scales_count", "fp8q_quantize", "fp8q_quantize_dual", "fp8q
                "fp8q_gemm_pow2", "fp8q_gemm_quantized", "fp8q_gemm_splitk_workspace", "fp8q_gemm_splitk",
                "fp8q_calibrate_clip_workspace", "fp8q_calibrate_clip", "fp8q_rmsnorm", "fp8q_rmsnorm_quantize",
                "fp8q_rmsnorm_backward_workspace", "fp8q_rmsnorm_backward", "fp8q_gemm_gated",
-               "fp8q_gemm_gated_quantized", "fp8q_gated_backward", "fp8q_requantize_transposed",
+               "fp8q_gemm_gated_workspace", "fp8q_gemm_gated_quantized", "fp8q_gated_backward",
+               "fp8q_requantize_transposed",
                "fp8q_policy_loss_workspace", "fp8q_token_logprobs", "fp8q_policy_loss")
 
 
@@ -155,7 +157,9 @@ def lib():
         L.fp8q_rmsnorm_backward.restype = i32
         L.fp8q_gemm_gated.argtypes = [p, p, i64, p, p, i64, i64, i64, i64, p, i64, p, i64, p]
         L.fp8q_gemm_gated.restype = i32
-        L.fp8q_gemm_gated_quantized.argtypes = [p, p, i64, p, p, i64, i64, i64, i64, p, i64, p, i64, p, p]
+        L.fp8q_gemm_gated_workspace.argtypes = [i64, i64, i64]
+        L.fp8q_gemm_gated_workspace.restype = i64
+        L.fp8q_gemm_gated_quantized.argtypes = [p, p, i64, p, p, i64, i64, i64, i64, p, i64, p, i64, p, p, i64, p]
         L.fp8q_gemm_gated_quantized.restype = i32
         L.fp8q_gated_backward.argtypes = [p, i64, p, i64, i64, i64, u32, p, i64, p, p, i64, p, p]
         L.fp8q_gated_backward.restype = i32
@@ -674,17 +678,22 @@ def gemm_gated(a, sa, b, sb, save=False, out=None, pre=None):
     return out, pre
 
 
-def gemm_gated_quantized(a, sa, b, sb, save=False, codes=None, scales=None, pre=None):
+def gemm_gated_quantized(a, sa, b, sb, save=False, codes=None, scales=None, pre=None, workspace=None):
     """gemm_gated() with H in 8 bits, the down projection's operand: returns
-    (codes, scales, pre), exactly quantize(h, BLOCK_1x128) of its h."""
-    r = _fast().gemm_gated_quantized(a, sa, b, sb, save, codes, scales, pre)
+    (codes, scales, pre), exactly quantize(h, BLOCK_1x128) of its h.
+    workspace: a uint8 CUDA tensor of fp8q_gemm_gated_workspace bytes (a new
+    one when None and the size needs one)."""
+    r = _fast().gemm_gated_quantized(a, sa, b, sb, save, codes, scales, pre, workspace)
     if r is not None:
         return _done(r, "fp8q_gemm_gated_quantized")
     M, F, K, pre, pc = _gated_operands(a, sa, b, sb, save, pre)
     codes = _given(codes, torch.uint8, "codes", (M, F), a.device)
     scales = _new_vector(scales, torch.float32, scales_count(M, F, BLOCK_1x128), "scales", a.device)
+    need = max(lib().fp8q_gemm_gated_workspace(M, F, K), 0)
+    workspace = _new_vector(workspace, torch.uint8, need, "workspace", a.device)
     st = lib().fp8q_gemm_gated_quantized(a.data_ptr(), sa.data_ptr(), _ld(a), b.data_ptr(), sb.data_ptr(), _ld(b), M, F,
-                                         K, *pc, codes.data_ptr(), _ld(codes), scales.data_ptr(), _stream(a))
+                                         K, *pc, codes.data_ptr(), _ld(codes), scales.data_ptr(),
+                                         workspace.data_ptr() if need else None, workspace.numel(), _stream(a))
     _check(st, "fp8q_gemm_gated_quantized")
     return codes, scales, pre
 

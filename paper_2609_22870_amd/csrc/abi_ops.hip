@@ -67,7 +67,8 @@ fp8q_status gated_args(const uint8_t* A, const float* sA, int64_t lda, const uin
   if (K % 128 || F % 128) return FP8Q_ERR_UNSUPPORTED;
   // the kernels' 32-bit offsets into B and the scales, and their tile counts
   if (2 * F * ldb >= ((int64_t)1 << 31) || M * (K / 128) >= ((int64_t)1 << 29)) return FP8Q_ERR_UNSUPPORTED;
-  if (((M + 127) / 128) * (F / 64) > ((int64_t)1 << 22)) return FP8Q_ERR_UNSUPPORTED;
+  if (((M + 127) / 128) * (F / 64) > ((int64_t)1 << 22) || M > (int64_t)65535 * 128) return FP8Q_ERR_UNSUPPORTED;
+  if (M * lda >= ((int64_t)1 << 31) && 256 * lda >= ((int64_t)1 << 31)) return FP8Q_ERR_UNSUPPORTED;
   if (!aligned(A, 16) || !aligned(B, 16) || lda % 16 || ldb % 16 || !aligned(sA, 4) || !aligned(sB, 4))
     return FP8Q_ERR_ALIGN;
   if (pre && (!aligned(pre, 8) || ldp % 4)) return FP8Q_ERR_ALIGN;
@@ -219,15 +220,28 @@ fp8q_status fp8q_gemm_gated(const uint8_t* A, const float* sA, int64_t lda, cons
   return from_hip(fp8q::launch_gemm_gated(g, false, stream_of(stream)));
 }
 
+int64_t fp8q_gemm_gated_workspace(int64_t M, int64_t F, int64_t K) {
+  if (M <= 0 || F <= 0 || K <= 0 || !dims_ok(M, F, K)) return -1;
+  return fp8q::gated_needs_bf16(M, F, K) ? 2 * M * F : 0;
+}
+
 fp8q_status fp8q_gemm_gated_quantized(const uint8_t* A, const float* sA, int64_t lda, const uint8_t* B, const float* sB,
                                       int64_t ldb, int64_t M, int64_t F, int64_t K, void* pre, int64_t ldp,
-                                      uint8_t* codes, int64_t ldq, float* scales, struct ihipStream_t* stream) {
+                                      uint8_t* codes, int64_t ldq, float* scales, void* workspace,
+                                      int64_t workspace_bytes, struct ihipStream_t* stream) {
   fp8q::GatedArgs g;
   const fp8q_status st = gated_args(A, sA, lda, B, sB, ldb, M, F, K, pre, ldp, g);
   if (!codes || !scales || (F > 0 && ldq < F)) return FP8Q_ERR_INVAL;
   if (st != FP8Q_OK) return st;
   if (ldq > kMaxDim) return FP8Q_ERR_UNSUPPORTED;
   if (!aligned(codes, 16) || ldq % 16 || !aligned(scales, 4)) return FP8Q_ERR_ALIGN;
+  if (const int64_t need = fp8q_gemm_gated_workspace(M, F, K)) {
+    if (!workspace || workspace_bytes < need) return FP8Q_ERR_INVAL;
+    if (!aligned(workspace, 16)) return FP8Q_ERR_ALIGN;
+    g.C = static_cast<uint16_t*>(workspace);
+    g.ldc = F;
+    g.c_aligned16 = 1;
+  }
   g.Cq = codes;
   g.Cs = scales;
   g.ldq = ldq;

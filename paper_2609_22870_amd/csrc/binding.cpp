@@ -44,6 +44,7 @@ struct Api {
   decltype(&fp8q_rmsnorm_backward_workspace) norm_workspace;
   decltype(&fp8q_rmsnorm_backward) rmsnorm_backward;
   decltype(&fp8q_gemm_gated) gemm_gated;
+  decltype(&fp8q_gemm_gated_workspace) gated_workspace;
   decltype(&fp8q_gemm_gated_quantized) gemm_gated_quantized;
   decltype(&fp8q_gated_backward) gated_backward;
   decltype(&fp8q_requantize_transposed) requantize_transposed;
@@ -526,11 +527,11 @@ bool truth(PyObject* o) {
 }
 
 // gemm_gated(a, sa, b, sb, save, out, pre) -> (out, pre) and
-// gemm_gated_quantized(a, sa, b, sb, save, codes, scales, pre) -> (codes,
-// scales, pre)
+// gemm_gated_quantized(a, sa, b, sb, save, codes, scales, pre, workspace) ->
+// (codes, scales, pre)
 template <bool QOUT>
 PyObject* py_gemm_gated(PyObject* m, PyObject* const* a, Py_ssize_t n) {
-  return guarded<QOUT ? 8 : 7>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+  return guarded<QOUT ? 9 : 7>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
     const Operands p = operands(api, a[0], a[1], FP8Q_BLOCK_1x128, a[2], a[3], FP8Q_BLOCK_128x128);
     PyObject* const given_pre = a[QOUT ? 7 : 6];
     if (p.N % 2) leave();
@@ -554,9 +555,19 @@ PyObject* py_gemm_gated(PyObject* m, PyObject* const* a, Py_ssize_t n) {
       const at::Tensor scales = vector_or_new(a[6], at::kFloat, ns, p.device);
       uint8_t* cp = codes.mutable_data_ptr<uint8_t>();
       float* sp = scales.mutable_data_ptr<float>();
+      const int64_t need = api.gated_workspace(p.M, F, p.K);
+      if (need < 0) leave();
+      at::Tensor ws;
+      void* wp = nullptr;
+      int64_t bytes = 0;
+      if (need > 0) {
+        ws = vector_or_new(a[8], at::kByte, need, p.device);
+        wp = ws.mutable_data_ptr();
+        bytes = ws.numel();
+      }
       const fp8q_status st = unlocked([&] {
         return api.gemm_gated_quantized(p.a, p.sa, p.lda, p.b, p.sb, p.ldb, p.M, F, p.K, pp, ldp, cp, codes.stride(0),
-                                        sp, p.stream);
+                                        sp, wp, bytes, p.stream);
       });
       if (st != FP8Q_OK) return PyLong_FromLong(st);
       return pack({give(a[5], codes), give(a[6], scales), kept()});

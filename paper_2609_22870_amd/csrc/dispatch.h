@@ -145,14 +145,14 @@ inline double tile_ns(const TileCost& c, double rounds, int64_t K) {
 }
 
 // The thin tile that takes the least time for the problems of one launch (of
-// one K), and that time.
-inline int thin_config(const GemmSize* probs, int count, double& ns) {
-  int best = 0;
-  for (int c = 0; c < kThinConfigs; ++c) {
+// one K), and that time; `first`: the smallest tile that may be chosen.
+inline int thin_config(const GemmSize* probs, int count, double& ns, int first = 0) {
+  int best = first;
+  for (int c = first; c < kThinConfigs; ++c) {
     int64_t tiles = 0;
     for (int i = 0; i < count; ++i) tiles += tile_count(probs[i], kThinM[c], kThinN[c]);
     const double t = tile_ns(kThinCost[c], (double)((tiles + kCUs - 1) / kCUs), probs[0].K);
-    if (c == 0 || t < ns) {
+    if (c == first || t < ns) {
       best = c;
       ns = t;
     }
@@ -228,6 +228,44 @@ inline GemmRoute gemm_splitk_route(int form, const GemmSize& s, int splits) {
   thin_config(&s, 1, thin);
   thin *= thin_from_memory(s) > 1.0 && s.M > 32 ? 1.4 : thin_from_memory(s);
   return thin < 7850 + 530.0 * (s.K / kBlockK) / splits + 811.0 * splits ? kThinTiles : kSplitK;
+}
+
+// The gated GEMM (s.N = 2 F rows of B): the kernel that a plain product of these
+// sizes takes, but for problems with more than one 128 x 128 tile per CU that
+// are no large tiles', which are few rows against a wide pair of weights here.
+// Up to 32 rows go to thin tiles (16 x 5120 x 17408 35.7 us, 128 x 128 tiles
+// 48.8; 32 rows 42.0 and 50.2), up to 64 to 64 x 64 tiles while those are fewer
+// than two and a half a CU (64 rows 49.2 and 54.9; 64 x 2048 x 25600, 3.1 a CU,
+// 27.1 and 25.8), and one round of 128 x 256 tiles takes less time than 128 x 128
+// ones from K = 1024 on (128 x 5120 x 17408 54.5 and 63.6 us; 128 x 512 x 17408
+// 9.0 and 8.8).
+enum { kHalfTiles = kSplitK + 1 };  // GatedRoute: a GemmRoute or 128 x 256 tiles
+
+inline int gated_route(const GemmSize& s) {
+  const GemmRoute r = gemm_route(2, s);  // 1x128 x 128x128
+  if (r != kMidTiles) return r;
+  if (s.M <= 32) return kThinTiles;
+  if (s.M <= 64 && tile_count(s, 64, 64) <= kCUs * 5 / 2) return kSmallTiles;
+  return tile_count(s, 128, 256) <= kCUs && s.K >= 1024 ? (int)kHalfTiles : (int)kMidTiles;
+}
+
+// Thin tiles of a gated product: at least a strip of 16 columns of each weight.
+// (Above one 128 x 128 tile per CU the estimates were not fitted: 16 x 32, or 32
+// x 32 for more than 16 rows, were the fastest there.)
+inline int gated_thin_config(const GemmSize& s) {
+  double ns;
+  if (tile_count(s, 128, 128) > kCUs) return s.M <= 16 ? kThin16x32 : kThin32x32;
+  return thin_config(&s, 1, ns, kThin16x32);
+}
+
+// H in 8 bits from one kernel: large tiles, and one round of 128 x 256 tiles in
+// place of 128 x 128 ones (whose 64 columns of H are half a unit).  Elsewhere H
+// goes to a workspace in bf16 and the quantizer follows: the tiles with whole units
+// take longer than that there (8 x 4096 x 12288: 40.7 us, 21.7 and about 3; 1039 x
+// 512 x 9984, 2.7 rounds: 28.4, 23.1 and 5).
+inline bool gated_through_bf16(const GemmSize& s) {
+  const int r = gated_route(s);
+  return r != kLargeTiles && r != kHalfTiles && !(r == kMidTiles && tile_count(s, 128, 256) <= kCUs);
 }
 
 // 1x128 quantization, plain layout: two rows a thread instead of eight.  Up

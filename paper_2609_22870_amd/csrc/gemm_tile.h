@@ -476,12 +476,13 @@ __device__ __forceinline__ void store_rows(const uint8_t* lds, uint16_t* dst, in
 // gate of columns h = wh + 16 j + 4 (lane / 16) + r in acc[i][j][r], j < TJ / 2, and
 // up of the same columns in acc[i][j + TJ / 2][r]; H is formed from the fp32 sums
 // and rounded once.  The kept pre-activations and H leave through LDS, one after
-// the other, in whole 16-byte chunks; H in 8 bits is the quantization of its
+// the other, in whole 16-byte chunks (`mine`: this wave's accumulators are the
+// tile's); H in 8 bits is the quantization of its
 // bf16 values, as fp8q_gemm_quantized's output is, so that both output types
 // stand for the same H.
 template <int BM, int BN, int TI, int TJ, int THREADS, bool QOUT>
-__device__ __forceinline__ void gated_epilogue(const GatedArgs& g, const v4f (&acc)[TI][TJ], uint8_t* lds, int64_t m0,
-                                               int64_t h0, int wm, int wh) {
+__device__ __forceinline__ void gated_epilogue(const GatedArgs& g, const v4f (&acc)[TI][TJ], bool mine, uint8_t* lds,
+                                               int64_t m0, int64_t h0, int wm, int wh) {
   constexpr int H = BN / 2;  // columns of the tile
   const int lane = threadIdx.x & 63;
   uint2 h[TI][TJ / 2];
@@ -501,15 +502,17 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& g, const v4f (&a
   __syncthreads();  // every wave is done with the operand stages
   if (g.pre) {
     constexpr int kMask = BN / 8 < 16 ? BN / 8 - 1 : 15;
+    if (mine) {
 #pragma unroll
-    for (int i = 0; i < TI; ++i)
+      for (int i = 0; i < TI; ++i)
 #pragma unroll
-      for (int j = 0; j < TJ; ++j) {
-        const int nt = (j < TJ / 2 ? 0 : H) + wh + (j % (TJ / 2)) * 16 + (lane >> 4) * 4;
-        const v4f a = acc[i][j];
-        stage(BN * 2, kMask, wm + i * 16 + (lane & 15), nt,
-              make_uint2(bf16x2_rne(a[0], a[1]), bf16x2_rne(a[2], a[3])));
-      }
+        for (int j = 0; j < TJ; ++j) {
+          const int nt = (j < TJ / 2 ? 0 : H) + wh + (j % (TJ / 2)) * 16 + (lane >> 4) * 4;
+          const v4f a = acc[i][j];
+          stage(BN * 2, kMask, wm + i * 16 + (lane & 15), nt,
+                make_uint2(bf16x2_rne(a[0], a[1]), bf16x2_rne(a[2], a[3])));
+        }
+    }
     __syncthreads();
     store_rows<BM, BN * 2, kMask, THREADS>(lds, g.pre + m0 * g.ldp, g.ldp, rows, g.pre_aligned16 != 0, [&](int c) {
       return h0 + (c < H / 8 ? c * 8 : g.N / 2 + c * 8 - H);
@@ -517,11 +520,13 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& g, const v4f (&a
     __syncthreads();
   }
   constexpr int kMask = H / 8 < 16 ? H / 8 - 1 : 15;
+  if (mine) {
 #pragma unroll
-  for (int i = 0; i < TI; ++i)
+    for (int i = 0; i < TI; ++i)
 #pragma unroll
-    for (int j = 0; j < TJ / 2; ++j)
-      stage(H * 2, kMask, wm + i * 16 + (lane & 15), wh + j * 16 + (lane >> 4) * 4, h[i][j]);
+      for (int j = 0; j < TJ / 2; ++j)
+        stage(H * 2, kMask, wm + i * 16 + (lane & 15), wh + j * 16 + (lane >> 4) * 4, h[i][j]);
+  }
   __syncthreads();
   if constexpr (QOUT) {
     static_assert(H % 128 == 0, "whole 1x128 units");
@@ -598,7 +603,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
   constexpr int kScaleA = Lds::kScaleA, kScaleB = Lds::kScaleB, kScaleStage = kScaleA + kScaleB;
   constexpr int kStages = Lds::kStages, kGroupBytes = Lds::kGroupBytes;
   static_assert(KS == 1 || (kStages > 2 && !QOUT), "K groups: the 64 x 64 tile");
-  static_assert(!GATED || (PAIR == kPairBlock && KS == 1 && !SPLITK && SUMS == 1), "gated: one plain tile");
+  static_assert(!GATED || (PAIR == kPairBlock && !SPLITK && SUMS == 1), "gated: plain tiles");
   const int wave_all = uniform(threadIdx.x >> 6);
   const int kg = KS > 1 ? uniform(wave_all / kWaves) : 0;  // K group
   uint8_t* const lds = lds_all + kg * kGroupBytes;
@@ -1137,8 +1142,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
 
   if constexpr (GATED) {
     static_assert(BM * BN * 2 <= kStages * kStage, "the pre-activations' tile must fit in the LDS stages");
-    gated_epilogue<BM, BN, TI, TJ, kWaves * 64, QOUT>(static_cast<const GatedArgs&>(g), acc, lds_all, m0, n0 / 2, wm,
-                                                      wn / 2);
+    gated_epilogue<BM, BN, TI, TJ, KS * kWaves * 64, QOUT>(static_cast<const GatedArgs&>(g), acc, kg == 0, lds_all, m0,
+                                                           n0 / 2, wm, wn / 2);
     return;
   }
 
@@ -1249,13 +1254,15 @@ struct ThinLds {
 };
 
 // The tile (tm, tn) of 16 TI x 16 TJ outputs; lds: ThinLds<TI, TJ>::kBytes.
-// QOUT: quantized output, with tiles of 32 x 128 (whole units).
-template <int PAIR, int TI, int TJ, bool QOUT, int FMT>
+// QOUT: quantized output, with tiles of 32 x 128 (whole units).  GATED: as in
+// gemm_tile; the first half of the tile's columns are the gate's.
+template <int PAIR, int TI, int TJ, bool QOUT, int FMT, bool GATED = false>
 __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int tm, int tn) {
   constexpr bool kBlockScaled = PAIR == kPairBlock || PAIR == kPairBlockK || PAIR == kPairBlockE8;
   constexpr bool kWeightBlocks = PAIR == kPairBlock || PAIR == kPairBlockE8;
   static_assert(TJ <= 8 && 8 % TJ == 0, "a tile's columns lie in one 128-column weight block");
-  constexpr int W = kThinWaves, kColScales = kWeightBlocks ? 1 : TJ * 4;
+  static_assert(!GATED || (PAIR == kPairBlock && !QOUT && TJ % 2 == 0), "gated: as many columns of both weights");
+  constexpr int W = kThinWaves, kColScales = GATED ? 2 : (kWeightBlocks ? 1 : TJ * 4);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int row = lane & 15, grp = lane >> 4;
   const int64_t m0 = (int64_t)tm * (TI * 16), n0 = (int64_t)tn * (TJ * 16);
@@ -1263,7 +1270,9 @@ __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int t
   const __amdgpu_buffer_rsrc_t rsB = make_rsrc(g.sB, (uint32_t)(g.sb_count * 4));
   uint8_t* const stage = lds + wave * ThinLds<TI, TJ>::kStage;  // B's rows, then A's
   const TileLoader<TI * 16, 1> ldA(g.A, g.lda, m0, g.M, 0);
-  const TileLoader<TJ * 16, 1> ldB(g.B, g.ldb, n0, g.N, 0);
+  constexpr int kHalf = GATED ? 2 : 1;
+  const TileLoader<TJ * 16 / kHalf, 1> ldB(g.B, g.ldb, n0 / kHalf, g.N, 0);
+  const TileLoader<TJ * 16 / kHalf, 1> ldUp(g.B, g.ldb, n0 / kHalf + (GATED ? g.N / 2 : 0), g.N, 0);
   const int kblocks = (int)(g.K / kBK);
 
   // K block kb to the stage, its scales to registers.  Scale offsets of rows
@@ -1275,13 +1284,15 @@ __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int t
 #pragma unroll
       for (int i = 0; i < TI; ++i) sa[i] = load_f32(rsA, ((int)m0 + i * 16 + row + kb * (int)g.sa_ld) * 4, 0);
     }
-    if constexpr (kWeightBlocks) sb[0] = load_f32(rsB, ((int)(n0 / 128) * kblocks + kb) * 4, 0);
+    if constexpr (kWeightBlocks) sb[0] = load_f32(rsB, ((int)(n0 / kHalf / 128) * kblocks + kb) * 4, 0);
+    if constexpr (GATED) sb[1] = load_f32(rsB, ((int)((n0 + g.N) / 256) * kblocks + kb) * 4, 0);
     if constexpr (PAIR == kPairBlockK) {
 #pragma unroll
       for (int q = 0; q < kColScales; ++q)
         sb[q] = load_f32(rsB, ((int)n0 + (q / 4) * 16 + grp * 4 + q % 4 + kb * (int)g.sb_ld) * 4, 0);
     }
     ldB.load(kb * kBK, stage, 0);
+    if constexpr (GATED) ldUp.load(kb * kBK, stage + TJ * 1024, 0);
     ldA.load(kb * kBK, stage + TJ * 2048, 0);
   };
 
@@ -1333,7 +1344,7 @@ __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int t
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             if constexpr (PAIR == kPairBlock)
-              acc[i][j][r] = __builtin_fmaf(p[r], ca[i] * cb[0], acc[i][j][r]);
+              acc[i][j][r] = __builtin_fmaf(p[r], ca[i] * cb[GATED && j >= TJ / 2 ? 1 : 0], acc[i][j][r]);
             else
               acc[i][j][r] = __builtin_fmaf(p[r] * ca[i], cb[j * 4 + r], acc[i][j][r]);
           }
@@ -1365,6 +1376,25 @@ __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int t
     }
     return v;
   };
+  if constexpr (GATED) {
+    const GatedArgs& gg = static_cast<const GatedArgs&>(g);
+    constexpr int H = TJ / 2;
+    for (int e = threadIdx.x; e < TI * H * 64; e += W * 64) {
+      const int l = e & 63, i = (e >> 6) / H, j = (e >> 6) % H;
+      const int64_t m = m0 + i * 16 + (l & 15), n = n0 / 2 + j * 16 + (l >> 4) * 4;
+      if (m >= g.M) continue;
+      const float4 a = sum_of((i * TJ + j) * 64 + l), b = sum_of((i * TJ + j + H) * 64 + l);
+      *reinterpret_cast<uint2*>(g.C + m * g.ldc + n) =
+          make_uint2(bf16x2_rne(gated_value(a.x, b.x), gated_value(a.y, b.y)),
+                     bf16x2_rne(gated_value(a.z, b.z), gated_value(a.w, b.w)));
+      if (gg.pre) {
+        uint16_t* const to = gg.pre + m * gg.ldp + n;
+        *reinterpret_cast<uint2*>(to) = make_uint2(bf16x2_rne(a.x, a.y), bf16x2_rne(a.z, a.w));
+        *reinterpret_cast<uint2*>(to + g.N / 2) = make_uint2(bf16x2_rne(b.x, b.y), bf16x2_rne(b.z, b.w));
+      }
+    }
+    return;
+  }
   if constexpr (QOUT) {
     // the bf16 tile to LDS (over the partials, once all are read), 256-byte
     // rows with chunk c at c ^ (row & 15), as store_quantized reads it

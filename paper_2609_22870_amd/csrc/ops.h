@@ -56,6 +56,9 @@ struct GatedArgs : GemmArgs {
   int64_t ldp = 0;
   int pre_aligned16 = 0;
 };
+// Quantized output of some sizes is made from H in bf16 (gated_needs_bf16): then C
+// is a workspace of M x F for it.
+bool gated_needs_bf16(int64_t M, int64_t F, int64_t K);
 hipError_t launch_gemm_gated(const GatedArgs& g, bool quantized, hipStream_t s);
 
 struct GatedBackwardArgs {
