@@ -535,8 +535,8 @@ fp8q_status fp8q_gemm_gated_quantized(const uint8_t *A, const float *sA,
  * where Mp is M rounded up to a multiple of 128; columns M .. Mp-1 of codes_t
  * are written as zeros.
  *   dh   bf16 [M][lddh];  pre  bf16 [M][ldp] as fp8q_gemm_gated wrote it
- * flags: FP8Q_E5M2, FP8Q_POW2_SCALE, both, or 0.  Shape rules: F % 128 == 0, M
- * <= 65535 x 128 (else FP8Q_ERR_UNSUPPORTED).  Alignment: dh, pre and both
+ * flags: FP8Q_E5M2, FP8Q_POW2_SCALE, both, or 0.  Shape rules: F % 128 == 0,
+ * fewer than 2^23 tiles of 128 x 128 (else FP8Q_ERR_UNSUPPORTED).  Alignment: dh, pre and both
  * code arrays 16-byte aligned, lddh and ldp multiples of 8, ldr and ldt of 16
  * (ldt >= Mp); scales 4-byte aligned.  The outputs must not overlap.
  */
@@ -556,7 +556,7 @@ fp8q_status fp8q_gated_backward(const void *dh, int64_t lddh, const void *pre,
  *   codes_t  E4M3 [cols][ldt], ldt >= Rp, rows rounded up to a multiple of
  *            128; columns rows .. Rp-1 are written as zeros
  *   scales_t [Rp/128][cols]
- * Shape rules: cols % 128 == 0, rows <= 65535 x 128 (else
+ * Shape rules: cols % 128 == 0, fewer than 2^23 tiles of 128 x 128 (else
  * FP8Q_ERR_UNSUPPORTED).  Alignment: both code arrays 16-byte aligned, ldc and
  * ldt multiples of 16; scales 4-byte aligned.  codes must not hold NaN.
  */

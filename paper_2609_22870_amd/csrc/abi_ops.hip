@@ -23,6 +23,9 @@ bool dims_ok(int64_t a, int64_t b, int64_t c = 1, int64_t d = 1, int64_t e = 1, 
 // a row, stay below 2^32 threads a launch.
 constexpr int64_t kMaxRows = ((int64_t)1 << 22) - 1;
 
+// Most 128 x 128 tiles of the backward operands: workgroups of up to 512 threads.
+constexpr int64_t kMaxTiles = ((int64_t)1 << 23) - 1;
+
 fp8q_status from_hip(hipError_t e) { return e == hipSuccess ? FP8Q_OK : FP8Q_ERR_HIP; }
 
 hipStream_t stream_of(struct ihipStream_t* s) { return reinterpret_cast<hipStream_t>(s); }
@@ -256,7 +259,7 @@ fp8q_status fp8q_gated_backward(const void* dh, int64_t lddh, const void* pre, i
   if ((flags & ~(unsigned)(FP8Q_POW2_SCALE | FP8Q_E5M2)) || M <= 0 || F <= 0) return FP8Q_ERR_INVAL;
   if (!dims_ok(M, F, lddh, ldp, ldr, ldt)) return FP8Q_ERR_UNSUPPORTED;
   if (lddh < F || ldp < 2 * F || ldr < 2 * F || ldt < (M + 127) / 128 * 128) return FP8Q_ERR_INVAL;
-  if (F % 128 || M > (int64_t)65535 * 128) return FP8Q_ERR_UNSUPPORTED;  // (rows of the grid)
+  if (F % 128 || (M + 127) / 128 * (F / 128) > kMaxTiles) return FP8Q_ERR_UNSUPPORTED;
   if (!aligned(dh, 16) || !aligned(pre, 16) || !aligned(codes_r, 16) || !aligned(codes_t, 16) || !aligned(scales_r, 4) ||
       !aligned(scales_t, 4) || lddh % 8 || ldp % 8 || ldr % 16 || ldt % 16)
     return FP8Q_ERR_ALIGN;
@@ -285,7 +288,7 @@ fp8q_status fp8q_requantize_transposed(const uint8_t* codes, int64_t ldc, const 
   if ((flags & ~(unsigned)FP8Q_POW2_SCALE) || rows <= 0 || cols <= 0) return FP8Q_ERR_INVAL;
   if (!dims_ok(rows, cols, ldc, ldt)) return FP8Q_ERR_UNSUPPORTED;
   if (ldc < cols || ldt < (rows + 127) / 128 * 128) return FP8Q_ERR_INVAL;
-  if (cols % 128 || rows > (int64_t)65535 * 128) return FP8Q_ERR_UNSUPPORTED;
+  if (cols % 128 || (rows + 127) / 128 * (cols / 128) > kMaxTiles) return FP8Q_ERR_UNSUPPORTED;
   if (!aligned(codes, 16) || !aligned(codes_t, 16) || !aligned(scales, 4) || !aligned(scales_t, 4) || ldc % 16 ||
       ldt % 16)
     return FP8Q_ERR_ALIGN;

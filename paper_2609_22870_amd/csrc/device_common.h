@@ -72,20 +72,37 @@ __device__ __forceinline__ UnitScale unit_scale_fmt(float amax, bool pow2) {
 // q F_max, RN(q + e r) is RN32(a / F_max) for every a in the normal range (checked
 // for every mantissa on the CPU); 1 / S is a reciprocal with one Newton step, good
 // to an ulp, which the quotient's own residual step corrects.  Units with a smaller
-// amax (zero among them) take the divisions.
-__device__ __noinline__ inline UnitScale small_unit_scale(float amax, float fmax) { return unit_scale(amax, fmax); }
+// amax (zero among them) take the division, and hand the quotient x and S both
+// times 2^64, exactly, so that every unit's quotients are the same three
+// instructions.
+struct CodeScale {
+  float s;     // S
+  float d, r;  // lift S and its reciprocal
+  float lift;  // 1 or 2^64: x / S = (lift x) / d
+};
+
+__device__ __noinline__ inline CodeScale small_code_scale(float amax, float fmax) {
+  const float s = amax / fmax;
+  if (s == 0.0f) return CodeScale{1.0f, 1.0f, 1.0f, 1.0f};
+  const float d = s * 0x1p64f;
+  return CodeScale{s, d, 1.0f / d, 0x1p64f};
+}
 
 template <bool E5>
-__device__ __forceinline__ UnitScale quick_unit_scale(float amax, bool pow2) {
-  if (pow2) return unit_scale_pow2(amax, E5 ? 16 : 9);
+__device__ __forceinline__ CodeScale code_scale(float amax, bool pow2) {
+  if (pow2) {
+    const float s = unit_scale_pow2(amax, E5 ? 16 : 9).s;
+    const float lift = s < 0x1p-90f ? 0x1p64f : 1.0f, d = s * lift;
+    return CodeScale{s, d, 1.0f / d, lift};
+  }
   constexpr float kMax = fp8_max<E5>(), kInv = 1.0f / kMax;
-  UnitScale u;
+  CodeScale u;
   const float q = amax * kInv;
-  u.s = __builtin_fmaf(__builtin_fmaf(-q, kMax, amax), kInv, q);
+  u.s = u.d = __builtin_fmaf(__builtin_fmaf(-q, kMax, amax), kInv, q);
   const float r = __builtin_amdgcn_rcpf(u.s);
   u.r = __builtin_fmaf(__builtin_fmaf(-u.s, r, 1.0f), r, r);
-  u.fast = true;
-  if (amax < 0x1p-64f) u = small_unit_scale(amax, kMax);
+  u.lift = 1.0f;
+  if (amax < 0x1p-64f) u = small_code_scale(amax, kMax);
   return u;
 }
 
@@ -128,6 +145,14 @@ __device__ __forceinline__ uint32_t e5m2_pack2(float a, float b, uint32_t old) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(ca, cb, (int)old, HI);
 }
 
+// The conversion without the clamp, for quotients by a CodeScale: |x / S| is at
+// most F_max (1 + 2^-23), which rounds to F_max.
+template <bool E5, bool HI>
+__device__ __forceinline__ uint32_t code_pack2(float a, float b, uint32_t old) {
+  return E5 ? (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(a, b, (int)old, HI)
+            : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)old, HI);
+}
+
 template <bool E5, bool HI>
 __device__ __forceinline__ uint32_t fp8_pack2(float a, float b, uint32_t old) {
   return E5 ? e5m2_pack2<HI>(a, b, old) : e4m3_pack2<HI>(a, b, old);
@@ -154,6 +179,18 @@ __device__ __forceinline__ float across_rows_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   v = fmaxf(v, __shfl_xor(v, 32, 64));
   return v;
+}
+
+// A value of the lane 16 (32) lanes away and this lane's, in either order: the
+// same pair in both lanes.  One instruction of the vector ALU each, where a shuffle
+// goes through LDS.
+__device__ __forceinline__ float2 with_lane16(float v) {
+  const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return make_float2(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float2 with_lane32(float v) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return make_float2(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
 __device__ __forceinline__ float wave_max(float v) { return across_rows_max(row16_max(v)); }

@@ -67,9 +67,9 @@ __device__ __forceinline__ float wave_sum(float v) {
   v += __int_as_float(__builtin_amdgcn_update_dpp(b, b, 0x141, 0xF, 0xF, false));
   b = __float_as_int(v);
   v += __int_as_float(__builtin_amdgcn_update_dpp(b, b, 0x140, 0xF, 0xF, false));
-  v += __shfl_xor(v, 16, 64);
-  v += __shfl_xor(v, 32, 64);
-  return v;
+  float2 p = with_lane16(v);
+  p = with_lane32(p.x + p.y);
+  return p.x + p.y;
 }
 
 // The row's sum (or maximum) over its THREADS threads; lds: one float a wave
@@ -88,15 +88,16 @@ __device__ __forceinline__ float row_reduce(float v, float* lds) {
   return v;
 }
 
-// Out of line: units with S < 2^-90 only.
-__device__ __noinline__ float slow_quotient(float x, float s) { return x / s; }
-
-__device__ __forceinline__ uint2 encode8(const float (&v)[8], const UnitScale& u) {
+__device__ __forceinline__ uint2 encode8(float (&v)[8], const CodeScale& u) {
+  if (__any(u.lift != 1.0f)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= u.lift;
+  }
   float q[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) q[e] = u.fast ? fast_quotient(v[e], u.s, u.r) : slow_quotient(v[e], u.s);
-  return make_uint2(e4m3_pack2<true>(q[2], q[3], e4m3_pack2<false>(q[0], q[1], 0u)),
-                    e4m3_pack2<true>(q[6], q[7], e4m3_pack2<false>(q[4], q[5], 0u)));
+  for (int e = 0; e < 8; ++e) q[e] = fast_quotient(v[e], u.d, u.r);
+  return make_uint2(code_pack2<false, true>(q[2], q[3], code_pack2<false, false>(q[0], q[1], 0u)),
+                    code_pack2<false, true>(q[6], q[7], code_pack2<false, false>(q[4], q[5], 0u)));
 }
 
 template <int THREADS, int VPT, int OUT>
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
   const float rstd = 1.0f / sqrtf(row_reduce<THREADS, false>(sum, lds) / (float)a.cols + a.eps);
   if (t == 0) a.rstd[r] = rstd;
 
-  UnitScale u{};
+  CodeScale u{};
   if constexpr (OUT == kNormRow) {
     float m = 0.0f;
 #pragma unroll
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e] * rstd * w[i][e]));
     }
-    u = quick_unit_scale<false>(row_reduce<THREADS, true>(m, lds + W), a.pow2 != 0);
+    u = code_scale<false>(row_reduce<THREADS, true>(m, lds + W), a.pow2 != 0);
     if (t == 0) a.scales[r] = u.s;
   }
 #pragma unroll
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
       float m = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
-      u = quick_unit_scale<false>(row16_max(m), a.pow2 != 0);
+      u = code_scale<false>(row16_max(m), a.pow2 != 0);
       if ((t & 15) == 0 && c < a.cols) a.scales[(c >> 7) * a.rows + r] = u.s;
     }
     if (c < a.cols) {
