@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace fp8q {
 
 constexpr float kE4M3Max = 448.0f;     // largest finite OCP E4M3 magnitude
@@ -88,7 +90,9 @@ __device__ __noinline__ inline CodeScale small_code_scale(float amax, float fmax
   return CodeScale{s, d, 1.0f / d, 0x1p64f};
 }
 
-template <bool E5>
+// EXACT: with a reciprocal good enough for fast_quotient; else as the hardware
+// gives it (an ulp).
+template <bool E5, bool EXACT = true>
 __device__ __forceinline__ CodeScale code_scale(float amax, bool pow2) {
   if (pow2) {
     const float s = unit_scale_pow2(amax, E5 ? 16 : 9).s;
@@ -100,7 +104,7 @@ __device__ __forceinline__ CodeScale code_scale(float amax, bool pow2) {
   const float q = amax * kInv;
   u.s = u.d = __builtin_fmaf(__builtin_fmaf(-q, kMax, amax), kInv, q);
   const float r = __builtin_amdgcn_rcpf(u.s);
-  u.r = __builtin_fmaf(__builtin_fmaf(-u.s, r, 1.0f), r, r);
+  u.r = EXACT ? __builtin_fmaf(__builtin_fmaf(-u.s, r, 1.0f), r, r) : r;
   u.lift = 1.0f;
   if (amax < 0x1p-64f) u = small_code_scale(amax, kMax);
   return u;
@@ -188,9 +192,30 @@ __device__ __forceinline__ float2 with_lane16(float v) {
   const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return make_float2(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
+// The larger magnitude of the two.
+__device__ __forceinline__ float magnitude_max(float2 p) {
+  const uint32_t a = __float_as_uint(p.x), b = __float_as_uint(p.y);
+  return __uint_as_float(a > b ? a : b);
+}
 __device__ __forceinline__ float2 with_lane32(float v) {
   const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return make_float2(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+// The maximum of magnitudes over the 16 lanes of a DPP row, as integers (the same
+// order): each step is one instruction, where a float maximum of shuffled bits
+// needs the move and a canonicalization of its own.
+__device__ __forceinline__ float row16_magnitude_max(float v) {
+  uint32_t m = __float_as_uint(v);
+  auto step = [&](auto ctrl) {
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, decltype(ctrl)::value, 0xF, 0xF, true);
+    m = m > o ? m : o;
+  };
+  step(std::integral_constant<int, 0xB1>{});   // quad [1,0,3,2]
+  step(std::integral_constant<int, 0x4E>{});   // quad [2,3,0,1]
+  step(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  step(std::integral_constant<int, 0x140>{});  // row_mirror
+  return __uint_as_float(m);
 }
 
 __device__ __forceinline__ float wave_max(float v) { return across_rows_max(row16_max(v)); }

@@ -20,6 +20,7 @@ namespace requant_detail {
 constexpr int kTile = 128;
 
 typedef float v2f __attribute__((ext_vector_type(2)));
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
 
 template <int COLS>
 struct Patch {
@@ -33,11 +34,13 @@ struct Shape {
   static constexpr int kGroups = 64 / kLanes;
 };
 
-// Four codes of the quotients by one unit's scale.
-template <bool E5>
+// Four codes of the quotients by one unit's scale.  EXACT: RN32(x / S).  Else x
+// times the reciprocal, at most two units in the last place from it, for x that
+// are themselves rounded results (a third of the vector instructions).
+template <bool E5, bool EXACT>
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, const CodeScale& u) {
-  return code_pack2<E5, true>(fast_quotient(c, u.d, u.r), fast_quotient(d, u.d, u.r),
-                              code_pack2<E5, false>(fast_quotient(a, u.d, u.r), fast_quotient(b, u.d, u.r), 0u));
+  auto q = [&](float x) { return EXACT ? fast_quotient(x, u.d, u.r) : x * u.r; };
+  return code_pack2<E5, true>(q(c), q(d), code_pack2<E5, false>(q(a), q(b), 0u));
 }
 
 // Workgroup b's tile, tiles numbered along the columns first.  Workgroup b runs on
@@ -54,26 +57,25 @@ __device__ __forceinline__ void tile_of(int tiles_c, int& tr, int& tc) {
 // Maximum over the lanes of a tile row.
 template <int COLS>
 __device__ __forceinline__ float row_max(float v) {
-  v = row16_max(v);
-  if constexpr (Shape<COLS>::kLanes > 16) {
-    const float2 p = with_lane16(v);
-    v = fmaxf(p.x, p.y);
-  }
-  return v;
+  v = row16_magnitude_max(v);
+  return Shape<COLS>::kLanes > 16 ? magnitude_max(with_lane16(v)) : v;
 }
 
 // The patch's 1x128 codes to rows row0 .. row0 + 7 (those below `rows`) from
 // column c on, and their scales, [cols / 128][rows] at block c / 128.
-template <int COLS, bool E5>
+template <int COLS, bool E5, bool EXACT>
 __device__ __forceinline__ void store_rows(const Patch<COLS>& p, bool pow2, int64_t row0, int64_t rows, int64_t c,
                                            uint8_t* codes, int64_t ldc, float* scales) {
   const int cc = threadIdx.x % Shape<COLS>::kLanes;
+  uint8_t* const to = codes + row0 * ldc + c;  // (row i: a scalar further on)
+  float* const st = scales + (c >> 7) * rows + row0;
+  const int left = (int)(rows - row0 < 8 ? rows - row0 : 8);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float m = 0.0f;
 #pragma unroll
     for (int j = 0; j < COLS; ++j) m = fmaxf(m, fabsf(p.v[i][j]));
-    const CodeScale u = code_scale<E5>(row_max<COLS>(m), pow2);
+    const CodeScale u = code_scale<E5, EXACT>(row_max<COLS>(m), pow2);
     const bool lifted = __any(u.lift != 1.0f);
     uint32_t w[COLS / 4];
 #pragma unroll
@@ -83,16 +85,14 @@ __device__ __forceinline__ void store_rows(const Patch<COLS>& p, bool pow2, int6
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] *= u.lift;
       }
-      w[j / 4] = codes4<E5>(v[0], v[1], v[2], v[3], u);
+      w[j / 4] = codes4<E5, EXACT>(v[0], v[1], v[2], v[3], u);
     }
-    const int64_t r = row0 + i;
-    if (r < rows) {
-      uint8_t* const to = codes + r * ldc + c;
+    if (i < left) {
       if constexpr (COLS == 8)
-        *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(to + i * ldc) = make_uint2(w[0], w[1]);
       else
-        *reinterpret_cast<uint32_t*>(to) = w[0];
-      if (cc == 0) scales[(c >> 7) * rows + r] = u.s;
+        *reinterpret_cast<uint32_t*>(to + i * ldc) = w[0];
+      if (cc == 0) st[i] = u.s;
     }
   }
 }
@@ -107,12 +107,8 @@ __device__ __forceinline__ void leave_col_max(const Patch<COLS>& p, float (*lds)
     float m = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(p.v[i][j]));
-    if constexpr (L == 16) {
-      const float2 q = with_lane16(m);
-      m = fmaxf(q.x, q.y);
-    }
-    const float2 q = with_lane32(m);
-    m = fmaxf(q.x, q.y);
+    if constexpr (L == 16) m = magnitude_max(with_lane16(m));
+    m = magnitude_max(with_lane32(m));
     if (lane < L) lds[threadIdx.x >> 6][cc * COLS + j] = m;
   }
 }
@@ -120,7 +116,7 @@ __device__ __forceinline__ void leave_col_max(const Patch<COLS>& p, float (*lds)
 // The patch's 128x1 codes, transposed, to LDS: line j of the tile (128 bytes, a
 // column's 128 tokens) holds in its eight-byte chunk g ^ (j / COLS % 16) the
 // tokens of row group g.  Then the scales, at scales + the tile's first column.
-template <int COLS, bool E5>
+template <int COLS, bool E5, bool EXACT>
 __device__ __forceinline__ void leave_columns(const Patch<COLS>& p, bool pow2, const float (*lds)[kTile],
                                               uint64_t* lines, float* scales) {
   constexpr int L = Shape<COLS>::kLanes, W = Shape<COLS>::kWaves;
@@ -129,8 +125,8 @@ __device__ __forceinline__ void leave_columns(const Patch<COLS>& p, bool pow2, c
   for (int j = 0; j < COLS; ++j) {
     float m = lds[0][cc * COLS + j];
 #pragma unroll
-    for (int w = 1; w < W; ++w) m = fmaxf(m, lds[w][cc * COLS + j]);
-    const CodeScale u = code_scale<E5>(m, pow2);
+    for (int w = 1; w < W; ++w) m = magnitude_max(make_float2(m, lds[w][cc * COLS + j]));
+    const CodeScale u = code_scale<E5, EXACT>(m, pow2);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = p.v[i][j];
@@ -138,7 +134,7 @@ __device__ __forceinline__ void leave_columns(const Patch<COLS>& p, bool pow2, c
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= u.lift;
     }
-    const uint32_t w[2] = {codes4<E5>(v[0], v[1], v[2], v[3], u), codes4<E5>(v[4], v[5], v[6], v[7], u)};
+    const uint32_t w[2] = {codes4<E5, EXACT>(v[0], v[1], v[2], v[3], u), codes4<E5, EXACT>(v[4], v[5], v[6], v[7], u)};
     lines[(cc * COLS + j) * 16 + (rg ^ (cc & 15))] = (uint64_t)w[0] | ((uint64_t)w[1] << 32);
     if (rg == 0) scales[cc * COLS + j] = u.s;
   }
@@ -156,6 +152,13 @@ __device__ __forceinline__ void store_lines(const uint64_t* lines, uint8_t* code
     *reinterpret_cast<uint4*>(codes_t + (c0 + j) * ldt + r0 + q * 16) =
         make_uint4((uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32));
   }
+}
+
+// Eight bytes that nothing reads again: they go past the caches, which keep what
+// is about to be read (4096 x 5120 gated gradient 62 -> 56 us).
+__device__ __forceinline__ uint2 read_once(const void* p) {
+  const v2u v = __builtin_nontemporal_load(static_cast<const v2u*>(p));
+  return make_uint2(v[0], v[1]);
 }
 
 // Two of the four codes in w (the low or the high 16 bits), as fp32.
@@ -186,14 +189,16 @@ __global__ __launch_bounds__(Shape<kRequantCols>::kThreads) void requant_kernel(
   const int64_t row0 = r0 + rg * 8, c = c0 + cc * C;
   uint2 w[8];
   float s[8];
+  const uint8_t* const pc = a.codes + row0 * a.ldc + c;
+  const float* const ps = a.scales + (int64_t)tc * a.rows + row0;
+  const int left = (int)(a.rows - row0 < 8 ? a.rows - row0 : 8);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int64_t r = row0 + i;
     w[i] = make_uint2(0u, 0u);
     s[i] = 0.0f;
-    if (r < a.rows) {
-      w[i] = *reinterpret_cast<const uint2*>(a.codes + r * a.ldc + c);
-      s[i] = a.scales[(int64_t)tc * a.rows + r];
+    if (i < left) {
+      w[i] = *reinterpret_cast<const uint2*>(pc + i * a.ldc);
+      s[i] = ps[i];
     }
   }
   Patch<C> p;
@@ -206,7 +211,7 @@ __global__ __launch_bounds__(Shape<kRequantCols>::kThreads) void requant_kernel(
   }
   leave_col_max<C>(p, lds);
   __syncthreads();
-  leave_columns<C, false>(p, a.pow2 != 0, lds, lines, a.scales_t + tr * a.cols + c0);
+  leave_columns<C, false, true>(p, a.pow2 != 0, lds, lines, a.scales_t + tr * a.cols + c0);
   __syncthreads();
   store_lines<C>(lines, a.codes_t, a.ldt, c0, r0);
 }
@@ -219,19 +224,9 @@ __global__ __launch_bounds__(Shape<kRequantCols>::kThreads) void requant_kernel(
 // multiple of 128 with zeros) for the weight gradient's.  6 bytes read and 4
 // written for each element of H.  A workgroup holds the tiles of dG and dU at
 // one place: 8 x 4 patches, so that both fit the registers of four waves per
-// SIMD.
-__device__ __forceinline__ float sigmoid(float g) {
-  // exp(-g) from exp2 with the product -g log2(e) in two parts, so that the
-  // result keeps fp32 accuracy at any g; past +-88 (where s is 1 or below the
-  // normal range) g is held there, which keeps every step finite
-  const float x = __builtin_amdgcn_fmed3f(-g, -88.0f, 88.0f);
-  constexpr float kLog2e = 0x1.715476p+0f, kLog2eLow = 0x1.4ae0bfp-26f, kLn2 = 0x1.62e430p-1f;
-  const float hi = x * kLog2e;
-  const float lo = __builtin_fmaf(x, kLog2eLow, __builtin_fmaf(x, kLog2e, -hi));
-  const float e = __builtin_amdgcn_exp2f(hi);
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo * kLn2, e));
-}
-
+// SIMD.  exp(-G) comes from one product and exp2, good to |G| 2^-24 of itself (G has
+// nine bits), and overflows to s = 0 as it should.
+constexpr float kLog2e = 0x1.715476p+0f;
 constexpr int kGatedCols = 4;
 
 template <bool E5>
@@ -245,14 +240,15 @@ __global__ __launch_bounds__(Shape<kGatedCols>::kThreads) void gated_backward_ke
   const int64_t r0 = (int64_t)tr * kTile, c0 = (int64_t)tc * kTile;
   const int64_t row0 = r0 + rg * 8, c = c0 + cc * C;
   uint2 g[8], u[8], d[8];
+  const uint16_t *const pg = a.pre + row0 * a.ldp + c, *const pu = pg + a.F, *const pd = a.dh + row0 * a.lddh + c;
+  const int left = (int)(a.M - row0 < 8 ? a.M - row0 : 8);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int64_t r = row0 + i;
     g[i] = u[i] = d[i] = make_uint2(0u, 0u);
-    if (r < a.M) {
-      g[i] = *reinterpret_cast<const uint2*>(a.pre + r * a.ldp + c);
-      u[i] = *reinterpret_cast<const uint2*>(a.pre + r * a.ldp + a.F + c);
-      d[i] = *reinterpret_cast<const uint2*>(a.dh + r * a.lddh + c);
+    if (i < left) {
+      g[i] = read_once(pg + i * a.ldp);
+      u[i] = read_once(pu + i * a.ldp);
+      d[i] = read_once(pd + i * a.lddh);
     }
   }
   Patch<C> dg, du;
@@ -264,20 +260,21 @@ __global__ __launch_bounds__(Shape<kGatedCols>::kThreads) void gated_backward_ke
       const float gv = j & 1 ? bf16_hi(gw[j >> 1]) : bf16_lo(gw[j >> 1]);
       const float uv = j & 1 ? bf16_hi(uw[j >> 1]) : bf16_lo(uw[j >> 1]);
       const float dv = j & 1 ? bf16_hi(dw[j >> 1]) : bf16_lo(dw[j >> 1]);
-      const float sig = sigmoid(gv), ds = dv * sig, dgs = ds * gv;
-      dg.v[i][j] = uv * __builtin_fmaf(dgs, 1.0f - sig, ds);
+      const float e = __builtin_amdgcn_exp2f(gv * -kLog2e), s = __builtin_amdgcn_rcpf(1.0f + e);
+      const float ds = dv * s, dgs = ds * gv;
+      dg.v[i][j] = uv * __builtin_fmaf(dgs, 1.0f - s, ds);
       du.v[i][j] = dgs;
     }
   }
   const bool pow2 = a.pow2 != 0;
   leave_col_max<C>(dg, lds[0]);
   leave_col_max<C>(du, lds[1]);
-  store_rows<C, E5>(dg, pow2, row0, a.M, c, a.codes_r, a.ldr, a.scales_r);
-  store_rows<C, E5>(du, pow2, row0, a.M, a.F + c, a.codes_r, a.ldr, a.scales_r);
+  store_rows<C, E5, false>(dg, pow2, row0, a.M, c, a.codes_r, a.ldr, a.scales_r);
+  store_rows<C, E5, false>(du, pow2, row0, a.M, a.F + c, a.codes_r, a.ldr, a.scales_r);
   __syncthreads();
   float* const st = a.scales_t + tr * 2 * a.F + c0;
-  leave_columns<C, E5>(dg, pow2, lds[0], lines[0], st);
-  leave_columns<C, E5>(du, pow2, lds[1], lines[1], st + a.F);
+  leave_columns<C, E5, false>(dg, pow2, lds[0], lines[0], st);
+  leave_columns<C, E5, false>(du, pow2, lds[1], lines[1], st + a.F);
   __syncthreads();
   store_lines<C>(lines[0], a.codes_t, a.ldt, c0, r0);
   store_lines<C>(lines[1], a.codes_t, a.ldt, a.F + c0, r0);
