@@ -13,9 +13,12 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/hip/impl/HIPCachingAllocatorMasqueradingAsCUDA.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPFunctions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cxxabi.h>
@@ -82,9 +85,18 @@ const at::Tensor& matrix(PyObject* o, at::ScalarType dtype) {
   return t;
 }
 
+// A new tensor.  On the current GPU from the caching allocator directly: a call
+// makes up to five, and at::empty's way through the dispatcher is half of each.
+at::Tensor fresh(c10::IntArrayRef sizes, at::ScalarType dtype, c10::Device device) {
+  if (device.type() == c10::DeviceType::CUDA && device.index() == c10::hip::current_device())
+    return at::detail::empty_generic(sizes, c10::hip::HIPCachingAllocatorMasqueradingAsCUDA::get(),
+                                     c10::DispatchKeySet(c10::DispatchKey::CUDA), dtype, std::nullopt);
+  return at::empty(sizes, at::TensorOptions().dtype(dtype).device(device));
+}
+
 // the same with that shape and device, or a new one for None
 at::Tensor matrix_or_new(PyObject* o, at::ScalarType dtype, int64_t rows, int64_t cols, c10::Device device) {
-  if (o == Py_None) return at::empty({rows, cols}, at::TensorOptions().dtype(dtype).device(device));
+  if (o == Py_None) return fresh({rows, cols}, dtype, device);
   const at::Tensor& t = matrix(o, dtype);
   if (t.size(0) != rows || t.size(1) != cols || t.device() != device) leave();
   return t;
@@ -100,7 +112,7 @@ const at::Tensor& vector(PyObject* o, at::ScalarType dtype, int64_t n, c10::Devi
 }
 
 at::Tensor vector_or_new(PyObject* o, at::ScalarType dtype, int64_t n, c10::Device device) {
-  if (o == Py_None) return at::empty({n}, at::TensorOptions().dtype(dtype).device(device));
+  if (o == Py_None) return fresh({n}, dtype, device);
   return vector(o, dtype, n, device);
 }
 

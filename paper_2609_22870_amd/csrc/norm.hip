@@ -24,6 +24,7 @@ namespace fp8q {
 namespace norm_detail {
 
 typedef float v2f __attribute__((ext_vector_type(2)));
+typedef unsigned int v4u __attribute__((ext_vector_type(4)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
@@ -44,6 +45,21 @@ __device__ __forceinline__ void widen(const uint4& p, float (&v)[8]) {
 __device__ __forceinline__ uint4 narrow(const float (&v)[8]) {
   return make_uint4(bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3]), bf16x2_rne(v[4], v[5]), bf16x2_rne(v[6], v[7]));
 }
+
+// 16 bytes that this pass alone touches (the streams in and out of a layer, which
+// nothing reads again before they have left the caches): past the caches, which
+// keep the codes for the GEMM that follows.
+__device__ __forceinline__ uint4 read_once(const uint16_t* p) {
+  const v4u v = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void write_once(uint16_t* p, const uint4& v) {
+  __builtin_nontemporal_store(v4u{v.x, v.y, v.z, v.w}, reinterpret_cast<v4u*>(p));
+}
+
+// From here on p is another value to the compiler: it would else keep the fp32
+// form of a held piece across the row's reduction, in twice the registers.
+__device__ __forceinline__ void forget(uint4& p) { asm volatile("" : "+v"(p.x), "+v"(p.y), "+v"(p.z), "+v"(p.w)); }
 
 __device__ __forceinline__ void load_weight(const void* weight, bool f32, int64_t c, float (&w)[8]) {
   if (f32) {
@@ -116,8 +132,8 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
     const int64_t c = ((int64_t)i * THREADS + t) * 8;
     x[i] = res[i] = make_uint4(0u, 0u, 0u, 0u);
     if (c < a.cols) {
-      x[i] = *reinterpret_cast<const uint4*>(a.x + r * a.ldx + c);
-      if (a.residual) res[i] = *reinterpret_cast<const uint4*>(a.residual + r * a.ldr + c);
+      x[i] = read_once(a.x + r * a.ldx + c);
+      if (a.residual) res[i] = read_once(a.residual + r * a.ldr + c);
     }
   }
 #pragma unroll
@@ -150,7 +166,7 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int64_t c = ((int64_t)i * THREADS + t) * 8;
-      if (c < a.cols) *reinterpret_cast<uint4*>(a.h + r * a.ldh + c) = x[i];
+      if (c < a.cols) write_once(a.h + r * a.ldh + c, x[i]);
     }
   }
   const float rstd = 1.0f / sqrtf(row_reduce<THREADS, false>(sum, lds) / (float)a.cols + a.eps);
@@ -195,82 +211,145 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
 // Backward pass.  With xhat = h rstd and g = dy w,
 //   dx = dres + rstd (g - xhat mean(g xhat)),   dw = sum over rows of dy xhat.
 // dx is the gradient of x and of the residual alike.  8 bytes an element (dy,
-// h, dres read, dx written; 6 without dres): a group of THREADS threads walks
-// rows group, group + groups, ..., each held in registers, and keeps its part of
-// dw there too; the parts go to a workspace and a second kernel adds them in
-// group order, so the sum is the same on every run.
+// h, dres read, dx written; 6 without dres): a walker of THREADS threads takes
+// rows walker, walker + walkers, ..., each held in registers, and keeps its part of
+// dw there too; a workgroup's parts (four walkers of one wave meet in LDS) go to a
+// workspace and a second kernel adds them in order, so the sum is the same on
+// every run.  The loads of the next row are in flight while a row is worked on.
+// 16384 x 4096 97 us (5.5 TB/s) with 512 workgroups; with 1024 110 us: their parts
+// of dw are as many bytes as an eighth of the rows.
 template <int THREADS, int VPT>
-__global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsnorm_backward_kernel(NormBackwardArgs a,
-                                                                                               int64_t groups) {
-  constexpr int kGroups = THREADS < kThreads ? kThreads / THREADS : 1;
+__global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsnorm_backward_kernel(NormBackwardArgs a) {
+  constexpr int kWalkers = THREADS < kThreads ? kThreads / THREADS : 1;  // of a workgroup
   constexpr int W = THREADS / 64;
+  // registers: rows of more than 8192 elements leave no room for the next row and
+  // for the weight, which is read again from L2 for every row
+  constexpr bool kNext = THREADS <= 512, kHoldWeight = THREADS <= 512;
   __shared__ float lds[2][W];
   const int t = threadIdx.x % THREADS;
-  const int64_t group = (int64_t)blockIdx.x * kGroups + threadIdx.x / THREADS;
-  if (group >= groups) return;  // a whole wave
-  float w[VPT][8], dw[VPT][8];
+  const int64_t walkers = (int64_t)gridDim.x * kWalkers;
+  const int64_t walker = (int64_t)blockIdx.x * kWalkers + threadIdx.x / THREADS;
+  float held[kHoldWeight ? VPT : 1][8], dw[VPT][8];
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int64_t c = ((int64_t)i * THREADS + t) * 8;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[i][e] = dw[i][e] = 0.0f;
-    if (c < a.cols) load_weight(a.weight, a.weight_f32 != 0, c, w[i]);
+    for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
+    if constexpr (kHoldWeight) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) held[i][e] = 0.0f;
+      if (c < a.cols) load_weight(a.weight, a.weight_f32 != 0, c, held[i]);
+    }
   }
-  int turn = 0;
-  for (int64_t r = group; r < a.rows; r += groups, turn ^= 1) {
-    uint4 dy[VPT], h[VPT], dres[VPT];
+  auto weight = [&](int i, float (&w)[8]) {
+    const int64_t c = ((int64_t)i * THREADS + t) * 8;
+    if constexpr (kHoldWeight) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = held[i][e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = 0.0f;
+      if (c < a.cols) load_weight(a.weight, a.weight_f32 != 0, c, w);
+    }
+  };
+  uint4 dy[kNext ? 2 : 1][VPT], h[kNext ? 2 : 1][VPT], dres[kNext ? 2 : 1][VPT];
+  auto fetch = [&](int64_t r, uint4 (&dy)[VPT], uint4 (&h)[VPT], uint4 (&dres)[VPT]) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int64_t c = ((int64_t)i * THREADS + t) * 8;
       dy[i] = h[i] = dres[i] = make_uint4(0u, 0u, 0u, 0u);
       if (c < a.cols) {
-        dy[i] = *reinterpret_cast<const uint4*>(a.dy + r * a.lddy + c);
-        h[i] = *reinterpret_cast<const uint4*>(a.h + r * a.ldh + c);
-        if (a.dres) dres[i] = *reinterpret_cast<const uint4*>(a.dres + r * a.ldres + c);
+        dy[i] = read_once(a.dy + r * a.lddy + c);
+        h[i] = read_once(a.h + r * a.ldh + c);
+        if (a.dres) dres[i] = read_once(a.dres + r * a.ldres + c);
       }
     }
+  };
+  // one row, held in dy, h and dres; turn: the row's part of lds (two in turn,
+  // so that one barrier a row is enough)
+  auto row = [&](int64_t r, int turn, uint4 (&dy)[VPT], uint4 (&h)[VPT], uint4 (&dres)[VPT]) {
     const float rstd = a.rstd[r];
     float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      float d[8], x[8];
+      float d[8], x[8], w[8];
       widen(dy[i], d);
       widen(h[i], x);
+      weight(i, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float xhat = x[e] * rstd;
-        dot = __builtin_fmaf(d[e] * w[i][e], xhat, dot);
+        dot = __builtin_fmaf(d[e] * w[e], xhat, dot);
         dw[i][e] = __builtin_fmaf(d[e], xhat, dw[i][e]);
       }
+      forget(dy[i]);
+      forget(h[i]);
     }
     const float mean = row_reduce<THREADS, false>(dot, lds[turn]) / (float)a.cols;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int64_t c = ((int64_t)i * THREADS + t) * 8;
-      float d[8], x[8], q[8];
+      float d[8], x[8], q[8], w[8];
       widen(dy[i], d);
       widen(h[i], x);
       widen(dres[i], q);
+      weight(i, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float g = __builtin_fmaf(-(x[e] * rstd), mean, d[e] * w[i][e]);
+        const float g = __builtin_fmaf(-(x[e] * rstd), mean, d[e] * w[e]);
         d[e] = __builtin_fmaf(rstd, g, q[e]);
       }
-      if (c < a.cols) *reinterpret_cast<uint4*>(a.dx + r * a.lddx + c) = narrow(d);
+      if (c < a.cols) write_once(a.dx + r * a.lddx + c, narrow(d));
     }
+  };
+  if constexpr (kNext) {
+    int64_t r = walker;
+    if (r < a.rows) fetch(r, dy[0], h[0], dres[0]);
+    for (; r < a.rows; r += 2 * walkers) {
+      const bool second = r + walkers < a.rows, third = r + 2 * walkers < a.rows;
+      if (second) fetch(r + walkers, dy[1], h[1], dres[1]);
+      row(r, 0, dy[0], h[0], dres[0]);
+      if (!second) break;
+      if (third) fetch(r + 2 * walkers, dy[0], h[0], dres[0]);
+      row(r + walkers, 1, dy[1], h[1], dres[1]);
+    }
+  } else {
+    int turn = 0;
+    for (int64_t r = walker; r < a.rows; r += walkers, turn ^= 1) {
+      fetch(r, dy[0], h[0], dres[0]);
+      row(r, turn, dy[0], h[0], dres[0]);
+    }
+  }
+  if constexpr (kWalkers > 1) {
+    __shared__ float parts[kWalkers - 1][VPT][8][64];
+    const int wave = threadIdx.x >> 6;
+    if (wave > 0) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) parts[wave - 1][i][e][t] = dw[i][e];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < kWalkers - 1; ++w)
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[i][e] += parts[w][i][e][t];
   }
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int64_t c = ((int64_t)i * THREADS + t) * 8;
     if (c < a.cols) {
-      float4* p = reinterpret_cast<float4*>(a.partials + group * a.cols + c);
+      float4* p = reinterpret_cast<float4*>(a.partials + blockIdx.x * a.cols + c);
       p[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
       p[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
     }
   }
 }
 
-// dweight from the groups' parts: a workgroup takes 64 columns, its sixteen
+// dweight from the workgroups' parts: a workgroup takes 64 columns, its sixteen
 // waves every sixteenth part each, eight loads in flight; LDS joins the waves
 // in order.
 constexpr int kReduceWaves = 16, kReduceDepth = 8;
@@ -303,8 +382,8 @@ __global__ __launch_bounds__(kReduceWaves * 64) void norm_weight_kernel(const fl
 }
 
 // f(THREADS, VPT) as integral constants: threads of a row and 16-byte pieces
-// of each.  One wave a row up to 1024 elements (no barrier), four up to 8192,
-// sixteen above.
+// of each.  One wave a row up to 1024 elements (no barrier), four up to 6144,
+// eight up to 8192, sixteen above.
 template <typename F>
 hipError_t with_shape(int64_t cols, F&& f) {
   using std::integral_constant;
@@ -313,7 +392,7 @@ hipError_t with_shape(int64_t cols, F&& f) {
   if (cols <= 2048) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   if (cols <= 4096) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
   if (cols <= 6144) return f(integral_constant<int, 256>{}, integral_constant<int, 3>{});
-  if (cols <= 8192) return f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  if (cols <= 8192) return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
   if (cols <= 16384) return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
   if (cols <= kMaxNormCols) return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
   return hipErrorInvalidValue;
@@ -344,16 +423,17 @@ hipError_t launch_rmsnorm(const NormArgs& a, NormOut out, hipStream_t s) {
 }
 
 int64_t norm_backward_groups(int64_t rows, int64_t cols) {
-  const int64_t most = cols <= 1024 ? 4096 : (cols <= 8192 ? 1024 : 256);
-  return rows < most ? rows : most;
+  // two workgroups of 256 threads a CU (16384 x 1024 29.0 us, with 1024 of them
+  // 35.5; 16384 x 4096 above), one of 512 or 1024 (8192 x 8192 97.9, with two 102)
+  const int64_t most = cols <= 6144 ? 512 : 256, ready = cols <= 1024 ? (rows + 3) / 4 : rows;
+  return ready < most ? ready : most;
 }
 
 hipError_t launch_rmsnorm_backward(const NormBackwardArgs& a, hipStream_t s) {
   const int64_t groups = norm_backward_groups(a.rows, a.cols);
   const hipError_t e = with_shape(a.cols, [&](auto threads, auto vpt) {
     constexpr int T = decltype(threads)::value, V = decltype(vpt)::value;
-    constexpr int block = T > kThreads ? T : kThreads, per = T < kThreads ? kThreads / T : 1;
-    rmsnorm_backward_kernel<T, V><<<dim3((unsigned)((groups + per - 1) / per)), block, 0, s>>>(a, groups);
+    rmsnorm_backward_kernel<T, V><<<dim3((unsigned)groups), T > kThreads ? T : kThreads, 0, s>>>(a);
     return hipGetLastError();
   });
   if (e != hipSuccess) return e;

@@ -45,7 +45,7 @@ struct NormBackwardArgs {
   float* dweight;
   float* partials;  // [norm_backward_groups(rows, cols)][cols]
 };
-// Groups of rows that sum their part of dweight each.
+// Workgroups that sum a part of dweight each.
 int64_t norm_backward_groups(int64_t rows, int64_t cols);
 hipError_t launch_rmsnorm_backward(const NormBackwardArgs& a, hipStream_t s);
 
