@@ -486,11 +486,25 @@ inline int split_parts(int64_t T, int64_t pieces, int& per) {
   return (int)parts;
 }
 
+// Whether rows are split over workgroups.  A row in one workgroup takes its CU's
+// time: GPU us of a call 7 + 1.05e-4 V (bf16) or 1.7e-4 V (fp32) with the gradient
+// and 3 + 6.2e-5 V without; split rows 10 (6) for one launch more, and then the
+// whole chip's time, 1.1e-6 (1.7e-6 fp32, 5.4e-7 without the gradient) T V.
+// Measured, one workgroup and split: 33 x 131072 bf16 22.6 and 15.0, 128 rows 26.2
+// and 27.9; 33 x 32000 10.8 and 11.4; log-probabilities of 64 x 131072 12.4 and
+// 10.5, of 128 13.4 and 16.4.
+inline bool split_rows(int64_t T, int64_t V, bool f32, bool grad) {
+  if (T >= kLossSplitRows) return false;
+  const double t = (double)T, v = (double)V;
+  if (!grad) return v * (6.2e-5 - 5.4e-7 * t) > 3.0;
+  return v * (f32 ? 1.7e-4 - 1.7e-6 * t : 1.05e-4 - 1.1e-6 * t) > 3.0;
+}
+
 template <bool F32, bool GRAD>
 hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
   constexpr int N = Piece<F32>::kN;
   const int64_t pieces = a.V / N + 1;
-  if (a.T < kLossSplitRows && pieces > 2 * kSplitThreads) {
+  if (split_rows(a.T, a.V, F32, GRAD)) {
     int per;
     const int parts = split_parts(a.T, pieces, per);
     const dim3 grid((unsigned)parts, (unsigned)a.T);
@@ -507,8 +521,10 @@ hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
   if (!GRAD) {
     if (pieces <= 4 * 256)
       row_kernel<F32, 256, 4, GRAD><<<grid, 256, 0, s>>>(a);
-    else
+    else if (pieces <= 8 * 512)
       row_kernel<F32, 512, 8, GRAD><<<grid, 512, 0, s>>>(a);
+    else
+      row_kernel<F32, 1024, 8, GRAD><<<grid, 1024, 0, s>>>(a);
   } else if (pieces <= 4 * 256) {
     row_kernel<F32, 256, 4, GRAD><<<grid, 256, 0, s>>>(a);
   } else if (pieces <= 8 * 256) {

@@ -100,7 +100,7 @@ struct LossArgs {
   float* partials;  // [T][kLossParts][4], for rows that are split
 };
 constexpr int kLossParts = 64;  // workgroups that share a row, at most
-constexpr int64_t kLossSplitRows = 256;  // rows fewer than this are split
+constexpr int64_t kLossSplitRows = 128;  // only rows fewer than this are split (see split_rows)
 hipError_t launch_logprobs(const LossArgs& a, hipStream_t s);
 hipError_t launch_policy_loss(const LossArgs& a, hipStream_t s);
 
