@@ -165,8 +165,10 @@ hipError_t launch_gemm_gated(const GatedArgs& g, bool quantized, hipStream_t s) 
 }  // namespace fp8q
 
 // The route of a gated product, for the tests (no part of the ABI): a GemmRoute
-// or kHalfTiles, plus 100 where quantized output goes through bf16.
+// or kHalfTiles, plus 10 times the thin tile, plus 100 where quantized output goes
+// through bf16.
 extern "C" int fp8q_gated_route(int64_t M, int64_t F, int64_t K) {
   const fp8q::GemmSize s{M, 2 * F, K};
-  return fp8q::gated_route(s) + (fp8q::gated_through_bf16(s) ? 100 : 0);
+  const int r = fp8q::gated_route(s);
+  return r + (r == fp8q::kThinTiles ? 10 * fp8q::gated_thin_config(s) : 0) + (fp8q::gated_through_bf16(s) ? 100 : 0);
 }
