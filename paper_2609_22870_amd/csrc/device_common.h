@@ -220,4 +220,25 @@ __device__ __forceinline__ float row16_magnitude_max(float v) {
 
 __device__ __forceinline__ float wave_max(float v) { return across_rows_max(row16_max(v)); }
 
+// The sum over 4, 8, 16 or 64 neighbouring lanes: every lane gets the same bits
+// (each step adds the same pair in both partners).
+template <int N = 64>
+__device__ __forceinline__ float wave_sum(float v) {
+  static_assert(N == 4 || N == 8 || N == 16 || N == 64);
+  auto step = [&](auto ctrl) {
+    const int b = __float_as_int(v);
+    v += __int_as_float(__builtin_amdgcn_update_dpp(b, b, decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  step(std::integral_constant<int, 0xB1>{});                          // quad [1,0,3,2]
+  step(std::integral_constant<int, 0x4E>{});                          // quad [2,3,0,1]
+  if constexpr (N >= 8) step(std::integral_constant<int, 0x141>{});   // row_half_mirror
+  if constexpr (N >= 16) step(std::integral_constant<int, 0x140>{});  // row_mirror
+  if constexpr (N == 64) {
+    float2 p = with_lane16(v);
+    p = with_lane32(p.x + p.y);
+    v = p.x + p.y;
+  }
+  return v;
+}
+
 }  // namespace fp8q

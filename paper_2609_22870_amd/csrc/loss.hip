@@ -83,47 +83,75 @@ struct Piece {
 // form of every held piece from the sums to the gradient, and spill.
 __device__ __forceinline__ void forget(uint4& p) { asm volatile("" : "+v"(p.x), "+v"(p.y), "+v"(p.z), "+v"(p.w)); }
 
-// Running sums of a softmax relative to 2^m: s = sum 2^(t - m), q = sum
-// 2^(t - m) (t - m), over t = x log2(e) / temperature; m = -inf: none yet.
+// The exponents of a row relative to that of its maximum m: u = x c - ref, one fused
+// multiply-add, with c = log2(e) / temperature and ref = RN(m c).  What ref is off by
+// is the same for every element, so it cancels; but from |m c| = 2^31 on it would
+// leave exp2's range (and m c that of fp32, in a row of nothing but the type's lowest
+// value, say).  There any other value is 2^7 or more below m's exponent, a weight of
+// nothing, so the scale is taken as the power of two that puts m c at 2^40: ref is
+// exact, m's own u 0 and every other's weight 0.  Relative to 0 where nothing is
+// finite.
+struct Exponent {
+  float c, ref;
+  __device__ __forceinline__ Exponent(float c_, float m) : c(c_) {
+    const float base = m == kNegInf ? 0.0f : m;
+    ref = base * c;
+    const bool wide = !in_range(ref);
+    if (__any(wide)) {
+      c = wide ? ldexpf(1.0f, min(41 - __builtin_amdgcn_frexp_expf(base), 126)) : c;
+      ref = base * c;
+    }
+  }
+  static __device__ __forceinline__ bool in_range(float ref) { return fabsf(ref) < 0x1p31f; }
+  __device__ __forceinline__ float operator()(float x) const { return __builtin_fmaf(x, c, -ref); }
+};
+
+// The exponent of x relative to m alone, at any range (x <= m, m above -inf).
+__device__ __forceinline__ float exponent_below(float x, float m, float c) {
+  const float ref = m * c;
+  return Exponent::in_range(ref) ? x * c - ref : (x - m) * c;
+}
+
+// Running sums of a softmax, over exponents relative to that of the maximum m: s =
+// sum 2^u, q = sum 2^u u; m = -inf: nothing finite yet.
 struct Sums {
   float m, s, q;
 };
 
-// The sums of both; each side's are taken to the larger maximum.
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b) {
+// Sums taken to the larger maximum m.
+__device__ __forceinline__ Sums moved(const Sums& a, float m, float c) {
+  // (one without a finite logit has nothing to move; one with +inf or NaN carries
+  // NaN in s)
+  const float d = a.m == kNegInf || a.m == m ? 0.0f : fmaxf(exponent_below(a.m, m, c), -1e30f);
+  const float f = __builtin_amdgcn_exp2f(d);
+  return Sums{m, a.s * f, f * __builtin_fmaf(a.s, d, a.q)};
+}
+
+// The sums of both, in either order.
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
   const float m = fmaxf(a.m, b.m);
-  // (a side without a finite logit has m = -inf and nothing to rescale; one
-  // with +inf or NaN carries NaN in s)
-  const float da = a.m == m ? 0.0f : a.m - m, db = b.m == m ? 0.0f : b.m - m;
-  const float fa = a.m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(da);
-  const float fb = b.m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(db);
-  Sums r;
-  r.m = m;
-  r.s = a.s * fa + b.s * fb;
-  r.q = fa * (a.m == kNegInf ? a.q : __builtin_fmaf(a.s, da, a.q)) +
-        fb * (b.m == kNegInf ? b.q : __builtin_fmaf(b.s, db, b.q));
-  return r;
+  const Sums x = moved(a, m, c), y = moved(b, m, c);
+  return Sums{m, x.s + y.s, x.q + y.q};
 }
 
-// The sums of one element t = x log2(e) / temperature (s is 1, and NaN for +inf
-// or NaN).
-__device__ __forceinline__ Sums single(float t) { return Sums{t, t == kNegInf ? 0.0f : 1.0f + (t - t), 0.0f}; }
-
-__device__ __forceinline__ Sums shuffled(const Sums& a, int mask) {
-  return Sums{__shfl_xor(a.m, mask, 64), __shfl_xor(a.s, mask, 64), __shfl_xor(a.q, mask, 64)};
+// The sums of one element (NaN for +inf or NaN).
+__device__ __forceinline__ Sums single(float x, float c) {
+  const float u = Exponent(c, x)(x), y = __builtin_amdgcn_exp2f(u);
+  return Sums{x, y, y * fmaxf(u, -1e30f)};
 }
 
-// The sums of N neighbouring lanes (every lane gets the same bits).
+// The sums of N neighbouring lanes (every lane gets the same bits), or of as many
+// that every N lanes hold again: all are taken to the common maximum, then added.
 template <int N = 64>
-__device__ __forceinline__ Sums wave_join(Sums a) {
-#pragma unroll
-  for (int mask = 1; mask < N; mask *= 2) a = join(a, shuffled(a, mask));
-  return a;
+__device__ __forceinline__ Sums wave_join(const Sums& a, float c) {
+  const float m = wave_max(a.m);
+  const Sums x = moved(a, m, c);
+  return Sums{m, wave_sum<N>(x.s), wave_sum<N>(x.q)};
 }
 
 // Adds K pieces to a thread's sums.
 template <bool F32, int K>
-__device__ __forceinline__ void add_pieces(const uint4* p, float c, Sums& a) {
+__device__ __forceinline__ void add_pieces(uint4* p, float c, Sums& a) {
   using P = Piece<F32>;
   float top = kNegInf;
 #pragma unroll
@@ -133,25 +161,22 @@ __device__ __forceinline__ void add_pieces(const uint4* p, float c, Sums& a) {
 #pragma unroll
     for (int e = 0; e < P::kN; ++e) top = fmaxf(top, v[e]);
   }
-  const float m = fmaxf(a.m, top * c);
-  const float ref = m == kNegInf ? 0.0f : m;
-  if (a.m != kNegInf) {
-    const float d = a.m - ref, f = __builtin_amdgcn_exp2f(d);
-    a.q = f * __builtin_fmaf(a.s, d, a.q);
-    a.s *= f;
-  }
-  a.m = m;
+  const float m = fmaxf(a.m, top);
+  a = moved(a, m, c);
+  const Exponent exponent(c, m);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
+    forget(p[k]);
     float v[P::kN];
     P::widen(p[k], v);
 #pragma unroll
     for (int e = 0; e < P::kN; ++e) {
-      const float u = __builtin_fmaf(v[e], c, -ref);
+      const float u = exponent(v[e]);
       const float x = __builtin_amdgcn_exp2f(u);
       a.s += x;
       a.q = __builtin_fmaf(x, fmaxf(u, -1e30f), a.q);  // (a logit of -inf adds 0, not 0 * -inf)
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -195,10 +220,12 @@ struct Token {
 
 __device__ __forceinline__ Token token_of(const LossArgs& a, int64_t row, const Sums& sums, float x, bool grad) {
   Token o{};
-  const float c = a.inv_temperature * kLog2e;
   const float log_s = logf(sums.s);
-  // (x c - m) ln 2 - log s; entropy = log s - ln 2 q / s, both relative to 2^m
-  o.logp = __builtin_fmaf(__builtin_fmaf(x, c, sums.m == kNegInf ? -0.0f : -sums.m), kLn2, -log_s);
+  // u ln 2 - log s; entropy = log s - ln 2 q / s, both relative to the maximum's exponent
+  const float c = a.inv_temperature * kLog2e;
+  const Exponent exponent(c, sums.m);
+  const float u = exponent.c == c ? exponent(x) : (x - sums.m) * c;
+  o.logp = __builtin_fmaf(u, kLn2, -log_s);
   o.entropy = log_s - kLn2 * (sums.q / sums.s);
   if (!grad) return o;
   const float low = a.clip ? (float)a.clip->l_new : a.clip_low, high = a.clip ? (float)a.clip->h_new : a.clip_high;
@@ -223,27 +250,27 @@ __device__ __forceinline__ bool counts(const LossArgs& a, int64_t row, int64_t t
   return token >= 0 && token < a.V && (!grad || a.weight[row] != 0.0f);
 }
 
-// A row's gradient: dx_j = (delta - p) k, p = 2^(x c - m) / s, ks = k / s.
+// A row's gradient: dx_j = (delta - p) k, p = 2^u / s, ks = k / s.
 template <bool F32>
 struct Gradient {
   using P = Piece<F32>;
   uint8_t* out;
   bool aligned;  // as the row of logits is, so that pieces go out whole
   int head, token;
-  float c, ref, k, ks;
+  Exponent u;
+  float k, ks;
   __device__ __forceinline__ Gradient(const LossArgs& a, int64_t row, const Row<F32>& x, int64_t tok, const Sums& sums,
-                                      float kk) {
+                                      float kk)
+      : u(a.inv_temperature * kLog2e, sums.m) {
     out = static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize;
     aligned = (((uintptr_t)out ^ (uintptr_t)x.base) & 15) == 0;
     head = x.head;
     token = (int)tok;
-    c = a.inv_temperature * kLog2e;
-    ref = sums.m == kNegInf ? 0.0f : sums.m;
     k = kk;
     ks = kk / sums.s;
   }
   __device__ __forceinline__ float of(float x, bool taken) const {
-    return (taken ? k : 0.0f) - ks * __builtin_amdgcn_exp2f(__builtin_fmaf(x, c, -ref));
+    return (taken ? k : 0.0f) - ks * __builtin_amdgcn_exp2f(u(x));
   }
   // of piece j0 + t, where that is below last
   __device__ __forceinline__ void put(const uint4& p, int j0, int last, unsigned t) const {
@@ -251,7 +278,7 @@ struct Gradient {
     float v[P::kN];
     P::widen(p, v);
 #pragma unroll
-    for (int e = 0; e < P::kN; ++e) v[e] = -ks * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], c, -ref));
+    for (int e = 0; e < P::kN; ++e) v[e] = -ks * __builtin_amdgcn_exp2f(u(v[e]));
     const unsigned at = (unsigned)(token - head - j0 * P::kN) - t * P::kN;
     if (at < (unsigned)P::kN) {
 #pragma unroll
@@ -287,7 +314,7 @@ __device__ __forceinline__ void store_zeros(const LossArgs& a, int64_t row, int6
 template <bool F32, int THREADS, int NV, bool GRAD>
 __global__ __launch_bounds__(THREADS) void row_kernel(LossArgs a) {
   using P = Piece<F32>;
-  constexpr int W = THREADS / 64, kChunk = NV % 4 == 0 ? 4 : 1;
+  constexpr int W = THREADS / 64, kChunk = NV % 4 == 0 ? 4 : 3;
   __shared__ Sums parts[W];
   __shared__ Token shared;
   const int t = threadIdx.x;
@@ -330,11 +357,11 @@ __global__ __launch_bounds__(THREADS) void row_kernel(LossArgs a) {
   }
   fetch(0);
   add();
-  if (edge >= 0) sums = join(sums, single(ev * c));
-  sums = wave_join(sums);
+  if (edge >= 0) sums = join(sums, single(ev, c), c);
+  sums = wave_join(sums, c);
   if ((t & 63) == 0) parts[t >> 6] = sums;
   __syncthreads();
-  sums = wave_join<W>(parts[t & (W - 1)]);
+  sums = wave_join<W>(parts[t & (W - 1)], c);
   if (t == 0) {
     const Token o = token_of(a, row, sums, mine, GRAD);
     a.logp[row] = o.logp;
@@ -388,13 +415,12 @@ __global__ __launch_bounds__(kSplitThreads) void split_sums_kernel(LossArgs a, i
     for (int i = 0; i < NV; i += 4) add_pieces<F32, 4>(held + i, c, sums);
   }
   const int edge = part == 0 ? x.edge(t) : -1;
-  if (edge >= 0) sums = join(sums, single(P::load(x.base, edge) * c));
-  sums = wave_join(sums);
+  if (edge >= 0) sums = join(sums, single(P::load(x.base, edge), c), c);
+  sums = wave_join(sums, c);
   if ((t & 63) == 0) shared[t >> 6] = sums;
   __syncthreads();
+  sums = wave_join<W>(shared[t & (W - 1)], c);
   if (t == 0) {
-#pragma unroll
-    for (int w = 1; w < W; ++w) sums = join(sums, shared[w]);
     float* const p = a.partials + (row * kLossParts + part) * 4;
     p[0] = sums.m;
     p[1] = sums.s;
@@ -411,7 +437,7 @@ __device__ __forceinline__ Sums joined(const LossArgs& a, int64_t row, int parts
     const float* const p = a.partials + (row * kLossParts + lane) * 4;
     s = Sums{p[0], p[1], p[2]};
   }
-  return wave_join(s);
+  return wave_join(s, a.inv_temperature * kLog2e);
 }
 
 // The log-probabilities of split rows: a wave a row.

@@ -72,22 +72,6 @@ __device__ __forceinline__ void load_weight(const void* weight, bool f32, int64_
   }
 }
 
-// Sum over the wave: every lane gets the same bits (each step adds the same
-// pair in both partners).
-__device__ __forceinline__ float wave_sum(float v) {
-  int b = __float_as_int(v);
-  v += __int_as_float(__builtin_amdgcn_update_dpp(b, b, 0xB1, 0xF, 0xF, false));
-  b = __float_as_int(v);
-  v += __int_as_float(__builtin_amdgcn_update_dpp(b, b, 0x4E, 0xF, 0xF, false));
-  b = __float_as_int(v);
-  v += __int_as_float(__builtin_amdgcn_update_dpp(b, b, 0x141, 0xF, 0xF, false));
-  b = __float_as_int(v);
-  v += __int_as_float(__builtin_amdgcn_update_dpp(b, b, 0x140, 0xF, 0xF, false));
-  float2 p = with_lane16(v);
-  p = with_lane32(p.x + p.y);
-  return p.x + p.y;
-}
-
 // The row's sum (or maximum) over its THREADS threads; lds: one float a wave
 // of the row, not in use by an earlier reduction that a thread may still read.
 template <int THREADS, bool MAX>

@@ -184,6 +184,68 @@ def test_masked_logits(T, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,V", [(20, 999), (5, 70001), (130, 40000)])
+def test_logits_at_the_ends_of_the_range(T, V, dtype):
+    """Rows of nothing but the type's lowest value (a mask that leaves nothing),
+    or its largest, are uniform; the largest among others takes everything; rows
+    beside them keep their results."""
+    b = batch(T, V, dtype, seed=43)
+    want = call(b, t=0.5)
+    top = torch.finfo(dtype).max
+    b["logits"][1], b["logits"][2], b["logits"][3] = -top, top, -top
+    b["logits"][3, 5] = top
+    b["tokens"][3] = 5
+    b["weight"][1:4] = 1.0
+    b["logp_old"][1:3] = b["logp_ref"][1:3] = -math.log(V)
+    b["logp_old"][3] = b["logp_ref"][3] = 0.0
+    ref = reference(b, t=0.5)
+    ref["tol"][1:4], ref["r2"][1:4] = 1e-5, 0.0
+    loss, dl, logp, entropy = call(b, t=0.5)
+    within(logp, ref["logp"], ref["tol"], "logp")
+    within(entropy, ref["entropy"], 4 * (1 + ref["r2"]) * ref["tol"], "entropy")
+    d = dl.cpu().to(F64)[1:4]
+    half = bf16_half(ref["dlogits"][1:4]) if dtype == torch.bfloat16 else 0.0
+    assert bool(((d - ref["dlogits"][1:4]).abs() <= 1e-4 * ref["dlogits"][1:4].abs() + half + 1e-30).all())
+    for i in range(T):
+        if not 1 <= i < 4:
+            same(dl[i], want[1][i], "row %d" % i)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,V", [(24, 999), (12, 70001), (130, 40000)])
+def test_large_logits(T, V, dtype):
+    """Rows far from 0, up to where a logit times log2(e) / t leaves fp32's range:
+    a common offset of the logits costs no accuracy (the fp32 exponent is relative
+    to the row's maximum), and of logits far apart the largest takes everything.
+    With an offset of 2^28 / t the fp32 exponents are up to 2^4 from the maximum's,
+    so a log-probability is good to 2^-24 of some 2^5, below 1e-5."""
+    b = batch(T, V, dtype, seed=47)
+    gen = torch.Generator().manual_seed(48)
+    rows = 0
+    for offset in (2.0**12, -(2.0**20), 2.0**24, -(2.0**27), 3e12, -1e37):
+        b["logits"][rows] = (offset + 4 * torch.randn(V, generator=gen, dtype=F64)).to(dtype).to(b["logits"].device)
+        rows += 1
+    for scale in (1e9, 1e12, 1e20, 4e37):
+        b["logits"][rows] = (scale * torch.randn(V, generator=gen, dtype=F64)).to(dtype).to(b["logits"].device)
+        b["tokens"][rows] = b["logits"][rows].argmax().to(b["tokens"].dtype)
+        rows += 1
+    b["weight"][:rows] = 1.0
+    logp = reference(b, t=0.5)["logp"][:rows].float()
+    b["logp_old"][:rows] = logp.to(b["logp_old"].device)
+    b["logp_ref"][:rows] = logp.to(b["logp_ref"].device)
+    ref = reference(b, t=0.5)
+    ref["tol"][:rows], ref["r2"][:rows] = 1e-5 + 2.0**-22 * ref["logp"][:rows].abs(), 0.0
+    loss, dl, logp, entropy = call(b, t=0.5)
+    within(logp, ref["logp"], ref["tol"], "logp")
+    within(entropy, ref["entropy"], 4 * (1 + ref["r2"]) * ref["tol"], "entropy")
+    assert math.isfinite(float(loss))
+    d = dl.cpu().to(F64)[:rows]
+    want = ref["dlogits"][:rows]
+    half = bf16_half(want) if dtype == torch.bfloat16 else 0.0
+    assert bool(((d - want).abs() <= 1e-4 * want.abs() + half + 1e-9 * want.abs().amax(dim=1, keepdim=True)).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("T,V", [(33, 1000), (6, 65537), (135, 20000)])
 def test_layouts(T, V, dtype):
     """Rows that start at any element (a slice of a wider buffer), gradients of
