@@ -411,8 +411,7 @@ __global__ __launch_bounds__(kSplitThreads) void split_sums_kernel(LossArgs a, i
     uint4 held[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) held[i] = x.piece(j0 + i * kSplitThreads, last, t);
-#pragma unroll
-    for (int i = 0; i < NV; i += 4) add_pieces<F32, 4>(held + i, c, sums);
+    add_pieces<F32, NV>(held, c, sums);
   }
   const int edge = part == 0 ? x.edge(t) : -1;
   if (edge >= 0) sums = join(sums, single(P::load(x.base, edge), c), c);
