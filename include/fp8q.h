@@ -500,11 +500,11 @@ fp8q_status fp8q_rmsnorm_backward(const void *dy, int64_t lddy, const void *h,
  * bytes (0 for the others, whose workspace may be null), 16-byte aligned,
  * overwritten.
  * Shape rules: K % 128 == 0, F % 128 == 0; 2 F ldb below 2^31, M K / 128 below
- * 2^29, M <= 65535 x 128, at most 2^22 tiles of 128 x 64 outputs, and 256 rows of
- * A below 2^31 bytes where all of them are not (else FP8Q_ERR_UNSUPPORTED).  Alignment: A, B and codes 16-byte aligned, lda, ldb
- * and ldq multiples of 16; H and pre 8-byte aligned with ldh and ldp multiples
- * of 4; scales 4-byte aligned.  The outputs must not overlap each other or an
- * input.
+ * 2^29, M <= 65535 x 128, at most 2^22 tiles of 128 x 64 outputs, and 256 rows
+ * of A below 2^31 bytes where all of them are not (else FP8Q_ERR_UNSUPPORTED).
+ * Alignment: A, B and codes 16-byte aligned, lda, ldb and ldq multiples of 16; H
+ * and pre 8-byte aligned with ldh and ldp multiples of 4; scales 4-byte aligned.
+ * The outputs must not overlap each other or an input.
  */
 fp8q_status fp8q_gemm_gated(const uint8_t *A, const float *sA, int64_t lda,
                             const uint8_t *B, const float *sB, int64_t ldb,
@@ -536,9 +536,9 @@ fp8q_status fp8q_gemm_gated_quantized(const uint8_t *A, const float *sA,
  * are written as zeros.
  *   dh   bf16 [M][lddh];  pre  bf16 [M][ldp] as fp8q_gemm_gated wrote it
  * flags: FP8Q_E5M2, FP8Q_POW2_SCALE, both, or 0.  Shape rules: F % 128 == 0,
- * fewer than 2^23 tiles of 128 x 128 (else FP8Q_ERR_UNSUPPORTED).  Alignment: dh, pre and both
- * code arrays 16-byte aligned, lddh and ldp multiples of 8, ldr and ldt of 16
- * (ldt >= Mp); scales 4-byte aligned.  The outputs must not overlap.
+ * fewer than 2^23 tiles of 128 x 128 (else FP8Q_ERR_UNSUPPORTED).  Alignment:
+ * dh, pre and both code arrays 16-byte aligned, lddh and ldp multiples of 8, ldr
+ * and ldt of 16 (ldt >= Mp); scales 4-byte aligned.  The outputs must not overlap.
  */
 fp8q_status fp8q_gated_backward(const void *dh, int64_t lddh, const void *pre,
                                 int64_t ldp, int64_t M, int64_t F,
@@ -585,9 +585,9 @@ int64_t fp8q_policy_loss_workspace(int64_t T, int64_t V);
  * +inf or of nothing but -inf gives NaN.
  * workspace: at least fp8q_policy_loss_workspace(T, V) bytes, 16-byte aligned,
  * overwritten (calls that share one must be ordered).  Shape rules: T below
- * 2^22, V below 2^31 (else FP8Q_ERR_UNSUPPORTED).  Alignment: logits to their type's
- * size (any ld >= V), tokens 8-byte, the others 4-byte aligned.
- * temperature > 0 (else FP8Q_ERR_INVAL).
+ * 2^22, V below 2^31 (else FP8Q_ERR_UNSUPPORTED).  Alignment: logits to their
+ * type's size (any ld >= V), tokens 8-byte, the others 4-byte aligned.
+ * temperature > 0, 1.5 / temperature within fp32 (else FP8Q_ERR_INVAL).
  */
 fp8q_status fp8q_token_logprobs(const void *logits, fp8q_dtype dtype,
                                 int64_t T, int64_t V, int64_t ld,
@@ -606,7 +606,7 @@ typedef struct fp8q_policy_batch {
                              response                                           */
   const float *w_tis;     /* truncated importance weights w; null: 1           */
   const float *logp_ref;  /* log-probabilities under the reference policy;
-                             null: no KL term                                   */
+                             null: no KL term (nor with beta 0: not read)       */
   const fp8q_clip_result *clip; /* bounds l_new and h_new, on the device, as
                              fp8q_calibrate_clip writes them; null: the next two */
   double clip_low, clip_high;   /* bounds of the ratio                          */

@@ -110,8 +110,8 @@ fp8q_status logit_args(const void* logits, fp8q_dtype dtype, int64_t T, int64_t 
                        double temperature, float* logp, float* entropy, void* workspace, int64_t workspace_bytes,
                        fp8q::LossArgs& a) {
   if (!logits || !tokens || !logp || !entropy || (dtype != FP8Q_BF16 && dtype != FP8Q_F32)) return FP8Q_ERR_INVAL;
-  const float inverse = (float)(1.0 / temperature);
-  if (T <= 0 || V <= 0 || ld < V || !(temperature > 0.0) || !isfinite(inverse) || inverse == 0.0f)
+  const float inverse = (float)(1.0 / temperature);  // (the kernels take log2(e) times it)
+  if (T <= 0 || V <= 0 || ld < V || !(temperature > 0.0) || !isfinite(1.5f * inverse) || inverse == 0.0f)
     return FP8Q_ERR_INVAL;
   if (T > kMaxRows || !dims_ok(T, V, ld)) return FP8Q_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < fp8q_policy_loss_workspace(T, V)) return FP8Q_ERR_INVAL;
@@ -341,7 +341,7 @@ fp8q_status fp8q_policy_loss(const void* logits, fp8q_dtype dtype, int64_t T, in
   a.adv = b.adv;
   a.weight = b.weight;
   a.w_tis = b.w_tis;
-  a.logp_ref = b.logp_ref;
+  a.logp_ref = (float)b.beta != 0.0f ? b.logp_ref : nullptr;
   a.clip = b.clip;
   a.clip_low = (float)b.clip_low;
   a.clip_high = (float)b.clip_high;

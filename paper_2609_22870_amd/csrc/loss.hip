@@ -230,14 +230,17 @@ __device__ __forceinline__ Token token_of(const LossArgs& a, int64_t row, const 
   if (!grad) return o;
   const float low = a.clip ? (float)a.clip->l_new : a.clip_low, high = a.clip ? (float)a.clip->h_new : a.clip_high;
   const float adv = a.adv[row], w = a.w_tis ? a.w_tis[row] : 1.0f, weight = a.weight[row];
-  const float r = expf(o.logp - a.logp_old[row]);
-  const float plain = r * adv, cut = fminf(fmaxf(r, low), high) * adv;
-  float l = -w * (plain > cut ? cut : plain);
-  float slope = plain > cut ? 0.0f : -w * plain;
+  // (the ratio stays finite, and w A is formed first: an advantage or weight of zero
+  // then takes nothing from a ratio that fp32 does not hold)
+  const float e = expf(o.logp - a.logp_old[row]), r = e > 0x1.fffffep127f ? 0x1.fffffep127f : e;
+  const float bounded = fminf(fmaxf(r, low), high), wa = w * adv;
+  const bool clipped = r * adv > bounded * adv;
+  float l = -wa * (clipped ? bounded : r);
+  float slope = clipped ? 0.0f : -wa * r;
   if (a.logp_ref) {
-    const float d = a.logp_ref[row] - o.logp, e = expm1f(d);
-    l += a.beta * (e - d);
-    slope -= a.beta * e;
+    const float d = a.logp_ref[row] - o.logp, m = expm1f(d);
+    l += a.beta * (m - d);
+    slope -= a.beta * m;
   }
   o.term = weight * l;
   o.k = weight * slope * a.inv_temperature;

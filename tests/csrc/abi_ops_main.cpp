@@ -214,6 +214,13 @@ int main() {
   fp8q_policy_batch b = batch();
   EXPECT(loss(&b), FP8Q_OK, 1);
   EXPECT(fp8q::last_loss.clip_low == 0.8f && fp8q::last_loss.inv_temperature == 1.0f ? 0 : 1, 0, 0);
+  b.logp_ref = at<float>();
+  EXPECT(loss(&b), FP8Q_OK, 1);  // (no KL term with a coefficient of zero)
+  EXPECT(fp8q::last_loss.logp_ref == nullptr ? 0 : 1, 0, 0);
+  b.beta = 0.1;
+  EXPECT(loss(&b), FP8Q_OK, 1);
+  EXPECT(fp8q::last_loss.logp_ref != nullptr ? 0 : 1, 0, 0);
+  b = batch();
   EXPECT(loss(nullptr), FP8Q_ERR_INVAL, 0);
   EXPECT(loss(&b, 0), FP8Q_ERR_INVAL, 0);
   EXPECT(loss(&b, 8, 1000, 999), FP8Q_ERR_INVAL, 0);
@@ -228,7 +235,7 @@ int main() {
   EXPECT(loss(&b, 8, 1000, 1000, FP8Q_BF16, 1 << 20, at<void>(), 999), FP8Q_ERR_INVAL, 0);
   EXPECT(loss(&b, 8, 1000, 1000, FP8Q_BF16, 1 << 20, at<void>(), WIDE), FP8Q_ERR_UNSUPPORTED, 0);
   EXPECT(loss(&b, 8, 1000, 1000, FP8Q_BF16, 1 << 20, at<void>(), 1000, at<void>(8)), FP8Q_ERR_ALIGN, 0);
-  const double bad_temperatures[] = {0.0, -1.0, (double)NAN, (double)INFINITY, 1e-60, 1e60};
+  const double bad_temperatures[] = {0.0, -1.0, (double)NAN, (double)INFINITY, 1e-60, 1e60, 3.5e-39};
   for (double t : bad_temperatures) {
     b = batch();
     b.temperature = t;

@@ -311,6 +311,26 @@ def test_every_branch_of_the_clip():
     check(call(b), ref, torch.float32)
 
 
+@pytest.mark.parametrize("T,V", [(9, 900), (9, 70001), (130, 900)])
+def test_ratios_past_the_range(T, V):
+    """exp(logp - logp_old) and exp(logp_ref - logp) past fp32: an advantage, an
+    importance weight or a KL coefficient of zero makes nothing of them, a clipped
+    ratio is cut as ever, and what has no finite value in fp32 is infinite."""
+    b = batch(T, V, torch.float32, seed=49)
+    b["weight"][:] = 0.5
+    b["logp_old"][:4] = -400.0
+    b["adv"][:4] = torch.tensor([0.0, 2.0, -2.0, 0.5])
+    b["w_tis"][2] = 0.0
+    b["logp_ref"][:4] = 400.0
+    ref = reference({k: v for k, v in b.items() if k != "logp_ref"}, beta=0.0)
+    check(call(b, beta=0.0), ref, torch.float32)
+    assert not bool(ref["dlogits"][:4].any())
+    b["w_tis"][2] = 1.0
+    loss, _, logp, _ = call(b, beta=0.0)
+    assert float(loss) == math.inf
+    within(logp, ref["logp"], ref["tol"], "logp")
+
+
 def test_gradient_against_differences():
     """The gradient along random directions against central differences of the
     64-bit loss."""
