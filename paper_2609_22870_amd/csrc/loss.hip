@@ -18,7 +18,8 @@
 // rows read what exceeds them again.  Too few rows to fill the chip are split
 // over several workgroups, which leave their sums in a workspace, and a second
 // kernel joins them.  Everything is in base 2 (one fused multiply-add and one
-// v_exp_f32 an element), with the temperature in the factor log2(e) / t.
+// v_exp_f32 an element), with the temperature in the factor log2(e) / t.  4096 x
+// 65536 bf16 with the gradient 211 us (5.1 TB/s), 64 x 131072 without 9.8.
 #include <type_traits>
 
 #include "device_common.h"
@@ -454,12 +455,53 @@ __global__ __launch_bounds__(64) void split_logprobs_kernel(LossArgs a, int part
   }
 }
 
+// The loss of split rows, by one workgroup: sixteen lanes a row join its parts and
+// form its token's term; the terms are added in float64, in a fixed order.
+__device__ __forceinline__ void split_loss(const LossArgs& a, int parts) {
+  __shared__ double terms[kLossSplitRows];
+  const int t = threadIdx.x, lane = t & 15;
+  const float c = a.inv_temperature * kLog2e;
+  if (t < kLossSplitRows) terms[t] = 0.0;
+  __syncthreads();
+  for (int r0 = 0; r0 < a.T; r0 += kSplitThreads / 16) {
+    const int64_t row = r0 + (t >> 4);
+    const bool live = row < a.T && counts(a, row, a.tokens[row], true);
+    const float4* const p = reinterpret_cast<const float4*>(a.partials) + row * kLossParts;
+    Sums s{kNegInf, 0.0f, 0.0f};
+    float x = 0.0f;
+    if (live) {
+      float4 v[kLossParts / 16];
+#pragma unroll
+      for (int i = 0; i < kLossParts / 16; ++i)
+        v[i] = lane + 16 * i < parts ? p[lane + 16 * i] : make_float4(kNegInf, 0.0f, 0.0f, 0.0f);
+      x = a.partials[row * kLossParts * 4 + 3];
+#pragma unroll
+      for (int i = 0; i < kLossParts / 16; ++i) s = join(s, Sums{v[i].x, v[i].y, v[i].z}, c);
+    }
+    const float m = row16_max(s.m);
+    s = moved(s, m, c);
+    s = Sums{m, wave_sum<16>(s.s), wave_sum<16>(s.q)};
+    if (live && lane == 0) terms[row] = (double)token_of(a, row, s, x, true).term;
+  }
+  __syncthreads();
+  for (int n = kLossSplitRows / 2; n > 0; n /= 2) {
+    if (t < n) terms[t] += terms[t + n];
+    __syncthreads();
+  }
+  if (t == 0) *a.loss = (float)terms[0];
+}
+
+// Workgroup (part, row + 1): the gradient of that part; (0, 0): the loss.
 template <bool F32>
 __global__ __launch_bounds__(kSplitThreads) void split_gradient_kernel(LossArgs a, int per, int parts) {
   using P = Piece<F32>;
   constexpr int NV = 4;
+  if (blockIdx.y == 0) {
+    if (blockIdx.x == 0) split_loss(a, parts);
+    return;
+  }
   const int t = threadIdx.x;
-  const int64_t part = blockIdx.x, row = blockIdx.y;
+  const int64_t part = blockIdx.x, row = (int64_t)blockIdx.y - 1;
   const int64_t token = a.tokens[row];
   const Row<F32> x(a.logits, a.ld, row, a.V);
   const int first = (int)part * per, last = first + per < x.full ? first + per : x.full;
@@ -467,7 +509,7 @@ __global__ __launch_bounds__(kSplitThreads) void split_gradient_kernel(LossArgs 
   if (!counts(a, row, token, true)) {
     store_zeros<F32, kSplitThreads>(a, row, x.head + first * P::kN, x.head + last * P::kN, t);
     if (edge >= 0) P::store(static_cast<uint8_t*>(a.dlogits) + row * a.ldd * P::kSize, edge, 0.0f);
-    if (part == 0 && t == 0) a.logp[row] = a.entropy[row] = a.terms[row] = 0.0f;
+    if (part == 0 && t == 0) a.logp[row] = a.entropy[row] = 0.0f;
     return;
   }
   const Sums sums = joined(a, row, parts);
@@ -475,7 +517,6 @@ __global__ __launch_bounds__(kSplitThreads) void split_gradient_kernel(LossArgs 
   if (part == 0 && t == 0) {
     a.logp[row] = o.logp;
     a.entropy[row] = o.entropy;
-    a.terms[row] = o.term;
   }
   const Gradient<F32> g(a, row, x, token, sums, o.k);
   for (int j0 = first; j0 < last; j0 += NV * kSplitThreads) {
@@ -515,12 +556,12 @@ inline int split_parts(int64_t T, int64_t pieces, int& per) {
 }
 
 // Whether rows are split over workgroups.  A row in one workgroup takes its CU's
-// time: GPU us of a call 7 + 1.05e-4 V (bf16) or 1.7e-4 V (fp32) with the gradient
-// and 3 + 6.2e-5 V without; split rows 10 (6) for one launch more, and then the
-// whole chip's time, 1.1e-6 (1.7e-6 fp32, 5.4e-7 without the gradient) T V.
-// Measured, one workgroup and split: 33 x 131072 bf16 22.6 and 15.0, 128 rows 26.2
-// and 27.9; 33 x 32000 10.8 and 11.4; log-probabilities of 64 x 131072 12.4 and
-// 10.5, of 128 13.4 and 16.4.
+// time: GPU us of a call 6 + 1.05e-4 V (bf16) or 1.7e-4 V (fp32) with the gradient
+// and 3 + 6.2e-5 V without; split rows 9 (6) for a launch more, and then the whole
+// chip's time, 1.1e-6 (1.7e-6 fp32, 5.4e-7 without the gradient) T V.  Measured, one
+// workgroup and split: 33 x 131072 bf16 20.7 and 13.3, 127 rows 24.8 and 33.2; 33 x
+// 32000 11.4 and 11.2; 33 x 131072 fp32 34.4 and 15.3, 64 x 32000 13.4 and 14.0;
+// log-probabilities of 64 x 131072 12.0 and 9.8, of 127 12.5 and 12.6.
 inline bool split_rows(int64_t T, int64_t V, bool f32, bool grad) {
   if (T >= kLossSplitRows) return false;
   const double t = (double)T, v = (double)V;
@@ -531,7 +572,7 @@ inline bool split_rows(int64_t T, int64_t V, bool f32, bool grad) {
 template <bool F32, bool GRAD>
 hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
   constexpr int N = Piece<F32>::kN;
-  const int64_t pieces = a.V / N + 1;
+  const int64_t pieces = a.V / N;  // (the most a row has)
   if (split_rows(a.T, a.V, F32, GRAD)) {
     int per;
     const int parts = split_parts(a.T, pieces, per);
@@ -540,11 +581,14 @@ hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (GRAD)
-      split_gradient_kernel<F32><<<grid, kSplitThreads, 0, s>>>(a, per, parts);
+      split_gradient_kernel<F32><<<dim3(grid.x, grid.y + 1), kSplitThreads, 0, s>>>(a, per, parts);
     else
       split_logprobs_kernel<<<dim3((unsigned)a.T), 64, 0, s>>>(a, parts);
     return hipGetLastError();
   }
+  // The smallest workgroup whose registers hold the row, so that a CU has more rows
+  // in flight (bf16: 4096 x 65536 in 512 threads 211 us, in 1024 279; 32768 in 256
+  // 113, in 512 132; log-probabilities of 4096 x 8192 in 256 threads 16, in 512 34).
   const dim3 grid((unsigned)a.T);
   if (!GRAD) {
     if (pieces <= 4 * 256)
@@ -579,7 +623,7 @@ hipError_t launch_logprobs(const LossArgs& a, hipStream_t s) {
 
 hipError_t launch_policy_loss(const LossArgs& a, hipStream_t s) {
   const hipError_t e = a.f32 ? launch_rows<true, true>(a, s) : launch_rows<false, true>(a, s);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || split_rows(a.T, a.V, a.f32, true)) return e;  // (split rows: the loss is there)
   loss_sum_kernel<<<1, kSumThreads, 0, s>>>(a.terms, a.T, a.loss);
   return hipGetLastError();
 }
