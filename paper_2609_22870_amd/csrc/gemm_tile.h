@@ -498,6 +498,9 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& g, const v4f (&a
   auto stage = [&](int row_bytes, int mask, int mt, int nt, const uint2& v) {
     *reinterpret_cast<uint2*>(lds + mt * row_bytes + (((nt >> 3) ^ (mt & mask)) << 4) + ((nt >> 2) & 1) * 8) = v;
   };
+  // Between one output and the next only LDS has to be settled: __syncthreads() would
+  // wait until the stores have left, too.
+  auto settle = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
   wait_vmem_all();  // no load may still be writing LDS
   __syncthreads();  // every wave is done with the operand stages
   if (g.pre) {
@@ -513,11 +516,11 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& g, const v4f (&a
                 make_uint2(bf16x2_rne(a[0], a[1]), bf16x2_rne(a[2], a[3])));
         }
     }
-    __syncthreads();
+    settle();
     store_rows<BM, BN * 2, kMask, THREADS>(lds, g.pre + m0 * g.ldp, g.ldp, rows, g.pre_aligned16 != 0, [&](int c) {
       return h0 + (c < H / 8 ? c * 8 : g.N / 2 + c * 8 - H);
     });
-    __syncthreads();
+    settle();
   }
   constexpr int kMask = H / 8 < 16 ? H / 8 - 1 : 15;
   if (mine) {
@@ -527,7 +530,7 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& g, const v4f (&a
       for (int j = 0; j < TJ / 2; ++j)
         stage(H * 2, kMask, wm + i * 16 + (lane & 15), wh + j * 16 + (lane >> 4) * 4, h[i][j]);
   }
-  __syncthreads();
+  settle();
   if constexpr (QOUT) {
     static_assert(H % 128 == 0, "whole 1x128 units");
     constexpr int kRowsPerPass = THREADS / (H / 8);
