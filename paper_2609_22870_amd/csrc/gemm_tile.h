@@ -437,16 +437,12 @@ __device__ __forceinline__ bool splitk_reduce(const GemmArgs& g, v4f (&acc)[TI][
   return true;
 }
 
-// silu(gate) up in fp32, exp(-gate) as exp2 of the product with log2(e) in two
-// parts (fp32 accuracy at any gate); past +-88, where silu is the gate or below
-// the normal range, the exponent is held.
+// silu(gate) up in fp32: exp(-gate) is exp2 of one product, good to some |gate| 2^-24
+// of itself (at most 2^-17, where the result is rounded to eight bits), 0 or infinite
+// past fp32's range, as it should be.
 __device__ __forceinline__ float gated_value(float gate, float up) {
-  constexpr float kLog2e = 0x1.715476p+0f, kLog2eLow = 0x1.4ae0bfp-26f, kLn2 = 0x1.62e430p-1f;
-  const float x = __builtin_amdgcn_fmed3f(-gate, -88.0f, 88.0f);
-  const float hi = x * kLog2e;
-  const float lo = __builtin_fmaf(x, kLog2eLow, __builtin_fmaf(x, kLog2e, -hi));
-  const float e = __builtin_amdgcn_exp2f(hi);
-  return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_fmaf(e, lo * kLn2, e)) * up;
+  constexpr float kLog2e = 0x1.715476p+0f;
+  return gate * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(gate * -kLog2e)) * up;
 }
 
 // A tile of bf16 rows of ROW_BYTES staged in LDS (16-byte chunk c of row m at c ^ (m
