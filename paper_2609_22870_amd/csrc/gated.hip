@@ -5,8 +5,8 @@
 // registers unless they are kept for the backward pass.  The kernels are those
 // of gemm_tile.h with a tile of B taken half from each weight.  Bound by the matrix
 // cores and the promotion beside them, as the plain GEMM: 16384 x 4096 x 12288 with
-// quantized output and kept pre-activations 1.6 ms (2.0 PFLOP/s); 8 tokens by the
-// weights, 16 us (6.3 TB/s).
+// quantized output and kept pre-activations 1.55 ms (2.1 PFLOP/s); 8 tokens by the
+// weights, 16 us (6.2 TB/s).
 #include "gemm_tile.h"
 
 namespace fp8q {
