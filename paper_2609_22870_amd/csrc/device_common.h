@@ -90,9 +90,7 @@ __device__ __noinline__ inline CodeScale small_code_scale(float amax, float fmax
   return CodeScale{s, d, 1.0f / d, 0x1p64f};
 }
 
-// EXACT: with a reciprocal good enough for fast_quotient; else as the hardware
-// gives it (an ulp).
-template <bool E5, bool EXACT = true>
+template <bool E5>
 __device__ __forceinline__ CodeScale code_scale(float amax, bool pow2) {
   if (pow2) {
     const float s = unit_scale_pow2(amax, E5 ? 16 : 9).s;
@@ -104,7 +102,7 @@ __device__ __forceinline__ CodeScale code_scale(float amax, bool pow2) {
   const float q = amax * kInv;
   u.s = u.d = __builtin_fmaf(__builtin_fmaf(-q, kMax, amax), kInv, q);
   const float r = __builtin_amdgcn_rcpf(u.s);
-  u.r = EXACT ? __builtin_fmaf(__builtin_fmaf(-u.s, r, 1.0f), r, r) : r;
+  u.r = __builtin_fmaf(__builtin_fmaf(-u.s, r, 1.0f), r, r);
   u.lift = 1.0f;
   if (amax < 0x1p-64f) u = small_code_scale(amax, kMax);
   return u;

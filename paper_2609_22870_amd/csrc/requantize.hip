@@ -34,12 +34,10 @@ struct Shape {
   static constexpr int kGroups = 64 / kLanes;
 };
 
-// Four codes of the quotients by one unit's scale.  EXACT: RN32(x / S).  Else x
-// times the reciprocal, at most two units in the last place from it, for x that
-// are themselves rounded results (a third of the vector instructions).
-template <bool E5, bool EXACT>
+// Four codes of the quotients by one unit's scale.
+template <bool E5>
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, const CodeScale& u) {
-  auto q = [&](float x) { return EXACT ? fast_quotient(x, u.d, u.r) : x * u.r; };
+  auto q = [&](float x) { return fast_quotient(x, u.d, u.r); };
   return code_pack2<E5, true>(q(c), q(d), code_pack2<E5, false>(q(a), q(b), 0u));
 }
 
@@ -63,7 +61,7 @@ __device__ __forceinline__ float row_max(float v) {
 
 // The patch's 1x128 codes to rows row0 .. row0 + 7 (those below `rows`) from
 // column c on, and their scales, [cols / 128][rows] at block c / 128.
-template <int COLS, bool E5, bool EXACT>
+template <int COLS, bool E5>
 __device__ __forceinline__ void store_rows(const Patch<COLS>& p, bool pow2, int64_t row0, int64_t rows, int64_t c,
                                            uint8_t* codes, int64_t ldc, float* scales) {
   const int cc = threadIdx.x % Shape<COLS>::kLanes;
@@ -75,7 +73,7 @@ __device__ __forceinline__ void store_rows(const Patch<COLS>& p, bool pow2, int6
     float m = 0.0f;
 #pragma unroll
     for (int j = 0; j < COLS; ++j) m = fmaxf(m, fabsf(p.v[i][j]));
-    const CodeScale u = code_scale<E5, EXACT>(row_max<COLS>(m), pow2);
+    const CodeScale u = code_scale<E5>(row_max<COLS>(m), pow2);
     const bool lifted = __any(u.lift != 1.0f);
     uint32_t w[COLS / 4];
 #pragma unroll
@@ -85,7 +83,7 @@ __device__ __forceinline__ void store_rows(const Patch<COLS>& p, bool pow2, int6
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] *= u.lift;
       }
-      w[j / 4] = codes4<E5, EXACT>(v[0], v[1], v[2], v[3], u);
+      w[j / 4] = codes4<E5>(v[0], v[1], v[2], v[3], u);
     }
     if (i < left) {
       if constexpr (COLS == 8)
@@ -116,7 +114,7 @@ __device__ __forceinline__ void leave_col_max(const Patch<COLS>& p, float (*lds)
 // The patch's 128x1 codes, transposed, to LDS: line j of the tile (128 bytes, a
 // column's 128 tokens) holds in its eight-byte chunk g ^ (j / COLS % 16) the
 // tokens of row group g.  Then the scales, at scales + the tile's first column.
-template <int COLS, bool E5, bool EXACT>
+template <int COLS, bool E5>
 __device__ __forceinline__ void leave_columns(const Patch<COLS>& p, bool pow2, const float (*lds)[kTile],
                                               uint64_t* lines, float* scales) {
   constexpr int L = Shape<COLS>::kLanes, W = Shape<COLS>::kWaves;
@@ -126,7 +124,7 @@ __device__ __forceinline__ void leave_columns(const Patch<COLS>& p, bool pow2, c
     float m = lds[0][cc * COLS + j];
 #pragma unroll
     for (int w = 1; w < W; ++w) m = magnitude_max(make_float2(m, lds[w][cc * COLS + j]));
-    const CodeScale u = code_scale<E5, EXACT>(m, pow2);
+    const CodeScale u = code_scale<E5>(m, pow2);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = p.v[i][j];
@@ -134,7 +132,7 @@ __device__ __forceinline__ void leave_columns(const Patch<COLS>& p, bool pow2, c
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= u.lift;
     }
-    const uint32_t w[2] = {codes4<E5, EXACT>(v[0], v[1], v[2], v[3], u), codes4<E5, EXACT>(v[4], v[5], v[6], v[7], u)};
+    const uint32_t w[2] = {codes4<E5>(v[0], v[1], v[2], v[3], u), codes4<E5>(v[4], v[5], v[6], v[7], u)};
     lines[(cc * COLS + j) * 16 + (rg ^ (cc & 15))] = (uint64_t)w[0] | ((uint64_t)w[1] << 32);
     if (rg == 0) scales[cc * COLS + j] = u.s;
   }
@@ -211,7 +209,7 @@ __global__ __launch_bounds__(Shape<kRequantCols>::kThreads) void requant_kernel(
   }
   leave_col_max<C>(p, lds);
   __syncthreads();
-  leave_columns<C, false, true>(p, a.pow2 != 0, lds, lines, a.scales_t + tr * a.cols + c0);
+  leave_columns<C, false>(p, a.pow2 != 0, lds, lines, a.scales_t + tr * a.cols + c0);
   __syncthreads();
   store_lines<C>(lines, a.codes_t, a.ldt, c0, r0);
 }
@@ -222,7 +220,7 @@ __global__ __launch_bounds__(Shape<kRequantCols>::kThreads) void requant_kernel(
 // both layouts of the backward GEMMs: codes per 1x128 unit for the data
 // gradient's, and transposed codes per 128x1 unit (the rows filled up to a
 // multiple of 128 with zeros) for the weight gradient's.  6 bytes read and 4
-// written for each element of H (16384 x 12288 412 us, 4.9 TB/s).  A workgroup holds the tiles of dG and dU at
+// written for each element of H (16384 x 12288 432 us, 4.7 TB/s).  A workgroup holds the tiles of dG and dU at
 // one place: 8 x 4 patches, so that both fit the registers of four waves per
 // SIMD.  exp(-G) comes from one product and exp2, good to |G| 2^-24 of itself (G has
 // nine bits), and overflows to s = 0 as it should.
@@ -269,12 +267,12 @@ __global__ __launch_bounds__(Shape<kGatedCols>::kThreads) void gated_backward_ke
   const bool pow2 = a.pow2 != 0;
   leave_col_max<C>(dg, lds[0]);
   leave_col_max<C>(du, lds[1]);
-  store_rows<C, E5, false>(dg, pow2, row0, a.M, c, a.codes_r, a.ldr, a.scales_r);
-  store_rows<C, E5, false>(du, pow2, row0, a.M, a.F + c, a.codes_r, a.ldr, a.scales_r);
+  store_rows<C, E5>(dg, pow2, row0, a.M, c, a.codes_r, a.ldr, a.scales_r);
+  store_rows<C, E5>(du, pow2, row0, a.M, a.F + c, a.codes_r, a.ldr, a.scales_r);
   __syncthreads();
   float* const st = a.scales_t + tr * 2 * a.F + c0;
-  leave_columns<C, E5, false>(dg, pow2, lds[0], lines[0], st);
-  leave_columns<C, E5, false>(du, pow2, lds[1], lines[1], st + a.F);
+  leave_columns<C, E5>(dg, pow2, lds[0], lines[0], st);
+  leave_columns<C, E5>(du, pow2, lds[1], lines[1], st + a.F);
   __syncthreads();
   store_lines<C>(lines[0], a.codes_t, a.ldt, c0, r0);
   store_lines<C>(lines[1], a.codes_t, a.ldt, a.F + c0, r0);
