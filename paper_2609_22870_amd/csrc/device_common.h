@@ -147,8 +147,18 @@ __device__ __forceinline__ uint32_t e5m2_pack2(float a, float b, uint32_t old) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(ca, cb, (int)old, HI);
 }
 
+// x lifted for its quotient by u, and held to F_max S: where S is an fp32 subnormal of
+// few bits it may be up to a third below amax / F_max, and larger quotients clamp.
+// (Units that need no lift have a normal S, within 2^-24 of amax / F_max.  A NaN stays.)
+template <bool E5>
+__device__ __forceinline__ float lifted_value(float x, const CodeScale& u) {
+  const float v = x * u.lift, most = fp8_max<E5>() * u.d;
+  return fabsf(v) > most ? copysignf(most, v) : v;
+}
+
 // The conversion without the clamp, for quotients by a CodeScale: |x / S| is at
-// most F_max (1 + 2^-23), which rounds to F_max.
+// most F_max (1 + 2^-23), which rounds to F_max, by S itself where it is normal and by
+// lifted_value where it is not.
 template <bool E5, bool HI>
 __device__ __forceinline__ uint32_t code_pack2(float a, float b, uint32_t old) {
   return E5 ? (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(a, b, (int)old, HI)

@@ -91,7 +91,7 @@ __device__ __forceinline__ float row_reduce(float v, float* lds) {
 __device__ __forceinline__ uint2 encode8(float (&v)[8], const CodeScale& u) {
   if (__any(u.lift != 1.0f)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= u.lift;
+    for (int e = 0; e < 8; ++e) v[e] = lifted_value<false>(v[e], u);
   }
   float q[8];
 #pragma unroll

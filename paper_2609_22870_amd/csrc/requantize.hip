@@ -81,7 +81,7 @@ __device__ __forceinline__ void store_rows(const Patch<COLS>& p, bool pow2, int6
       float v[4] = {p.v[i][j], p.v[i][j + 1], p.v[i][j + 2], p.v[i][j + 3]};
       if (lifted) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] *= u.lift;
+        for (int e = 0; e < 4; ++e) v[e] = lifted_value<E5>(v[e], u);
       }
       w[j / 4] = codes4<E5>(v[0], v[1], v[2], v[3], u);
     }
@@ -130,7 +130,7 @@ __device__ __forceinline__ void leave_columns(const Patch<COLS>& p, bool pow2, c
     for (int i = 0; i < 8; ++i) v[i] = p.v[i][j];
     if (__any(u.lift != 1.0f)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= u.lift;
+      for (int i = 0; i < 8; ++i) v[i] = lifted_value<E5>(v[i], u);
     }
     const uint32_t w[2] = {codes4<E5>(v[0], v[1], v[2], v[3], u), codes4<E5>(v[4], v[5], v[6], v[7], u)};
     lines[(cc * COLS + j) * 16 + (rg ^ (cc & 15))] = (uint64_t)w[0] | ((uint64_t)w[1] << 32);
