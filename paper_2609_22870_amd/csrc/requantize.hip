@@ -220,11 +220,13 @@ __global__ __launch_bounds__(Shape<kRequantCols>::kThreads) void requant_kernel(
 // both layouts of the backward GEMMs: codes per 1x128 unit for the data
 // gradient's, and transposed codes per 128x1 unit (the rows filled up to a
 // multiple of 128 with zeros) for the weight gradient's.  6 bytes read and 4
-// written for each element of H (16384 x 12288 432 us, 4.7 TB/s).  A workgroup holds the tiles of dG and dU at
+// written for each element of H (16384 x 12288 430 us, 4.7 TB/s).  A workgroup holds the tiles of dG and dU at
 // one place: 8 x 4 patches, so that both fit the registers of four waves per
-// SIMD.  exp(-G) comes from one product and exp2, good to |G| 2^-24 of itself (G has
-// nine bits), and overflows to s = 0 as it should.
-constexpr float kLog2e = 0x1.715476p+0f;
+// SIMD.  log2(e) is kLog2e, sixteen bits whose product with a bf16 G is exact, and a
+// rest of which kRest is ln 2 times: exp(-G) = 2^(-G kLog2e) (1 - G kRest), good to fp32 (at
+// |G| = 87 the next term is 2^-23), and overflows to s = 0 as it should.  (One rounded
+// product was off by |G| 2^-24 of the value.)
+constexpr float kLog2e = 0x1.7154p+0f, kRest = 0x1.480fb6p-18f;
 constexpr int kGatedCols = 4;
 
 template <bool E5>
@@ -258,7 +260,8 @@ __global__ __launch_bounds__(Shape<kGatedCols>::kThreads) void gated_backward_ke
       const float gv = j & 1 ? bf16_hi(gw[j >> 1]) : bf16_lo(gw[j >> 1]);
       const float uv = j & 1 ? bf16_hi(uw[j >> 1]) : bf16_lo(uw[j >> 1]);
       const float dv = j & 1 ? bf16_hi(dw[j >> 1]) : bf16_lo(dw[j >> 1]);
-      const float e = __builtin_amdgcn_exp2f(gv * -kLog2e), s = __builtin_amdgcn_rcpf(1.0f + e);
+      const float e = __builtin_amdgcn_exp2f(gv * -kLog2e) * __builtin_fmaf(gv, -kRest, 1.0f);
+      const float s = __builtin_amdgcn_rcpf(1.0f + e);
       const float ds = dv * s, dgs = ds * gv;
       dg.v[i][j] = uv * __builtin_fmaf(dgs, 1.0f - s, ds);
       du.v[i][j] = dgs;
