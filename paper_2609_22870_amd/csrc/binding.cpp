@@ -13,11 +13,14 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/Context.h>
 #include <ATen/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/impl/HIPCachingAllocatorMasqueradingAsCUDA.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <ATen/ops/empty.h>
+#include <ATen/record_function.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/hip/HIPFunctions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -85,10 +88,19 @@ const at::Tensor& matrix(PyObject* o, at::ScalarType dtype) {
   return t;
 }
 
-// A new tensor.  On the current GPU from the caching allocator directly: a call
-// makes up to five, and at::empty's way through the dispatcher is half of each.
+// Whether nothing but the allocator takes part in at::empty: no dispatch mode or
+// transform, no profiler or other observer of calls, no fill of new memory.
+bool plain_allocation() {
+  const at::Context& c = at::globalContext();
+  return (c10::impl::tls_local_dispatch_key_set().included_ - c10::default_included_set).empty() &&
+         !at::hasCallbacks() && !(c.deterministicAlgorithms() && c.deterministicFillUninitializedMemory());
+}
+
+// at::empty.  On the current GPU from the caching allocator directly where that is
+// all at::empty would do: a call makes up to five tensors, and the way through the
+// dispatcher is half of each.
 at::Tensor fresh(c10::IntArrayRef sizes, at::ScalarType dtype, c10::Device device) {
-  if (device.type() == c10::DeviceType::CUDA && device.index() == c10::hip::current_device())
+  if (device.type() == c10::DeviceType::CUDA && device.index() == c10::hip::current_device() && plain_allocation())
     return at::detail::empty_generic(sizes, c10::hip::HIPCachingAllocatorMasqueradingAsCUDA::get(),
                                      c10::DispatchKeySet(c10::DispatchKey::CUDA), dtype, std::nullopt);
   return at::empty(sizes, at::TensorOptions().dtype(dtype).device(device));
