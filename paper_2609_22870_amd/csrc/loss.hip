@@ -583,7 +583,7 @@ hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
     split_sums_kernel<F32, GRAD><<<grid, kSplitThreads, 0, s>>>(a, per);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (GRAD)
+    if constexpr (GRAD)
       split_gradient_kernel<F32><<<dim3(grid.x, grid.y + 1), kSplitThreads, 0, s>>>(a, per, parts);
     else
       split_logprobs_kernel<<<dim3((unsigned)a.T), 64, 0, s>>>(a, parts);
@@ -593,25 +593,25 @@ hipError_t launch_rows(const LossArgs& a, hipStream_t s) {
   // in flight (bf16: 4096 x 65536 in 512 threads 211 us, in 1024 279; 32768 in 256
   // 113, in 512 132, all with cached stores; log-probabilities of 4096 x 8192 in 256 threads 16, in 512 34).
   const dim3 grid((unsigned)a.T);
-  if (!GRAD) {
+  if constexpr (!GRAD) {
     if (pieces <= 4 * 256)
-      row_kernel<F32, 256, 4, GRAD><<<grid, 256, 0, s>>>(a);
+      row_kernel<F32, 256, 4, false><<<grid, 256, 0, s>>>(a);
     else if (pieces <= 8 * 512)
-      row_kernel<F32, 512, 8, GRAD><<<grid, 512, 0, s>>>(a);
+      row_kernel<F32, 512, 8, false><<<grid, 512, 0, s>>>(a);
     else
-      row_kernel<F32, 1024, 8, GRAD><<<grid, 1024, 0, s>>>(a);
+      row_kernel<F32, 1024, 8, false><<<grid, 1024, 0, s>>>(a);
   } else if (pieces <= 4 * 256) {
-    row_kernel<F32, 256, 4, GRAD><<<grid, 256, 0, s>>>(a);
+    row_kernel<F32, 256, 4, true><<<grid, 256, 0, s>>>(a);
   } else if (pieces <= 8 * 256) {
-    row_kernel<F32, 256, 8, GRAD><<<grid, 256, 0, s>>>(a);
+    row_kernel<F32, 256, 8, true><<<grid, 256, 0, s>>>(a);
   } else if (pieces <= 16 * 256) {
-    row_kernel<F32, 256, 16, GRAD><<<grid, 256, 0, s>>>(a);
+    row_kernel<F32, 256, 16, true><<<grid, 256, 0, s>>>(a);
   } else if (pieces <= 16 * 512) {
-    row_kernel<F32, 512, 16, GRAD><<<grid, 512, 0, s>>>(a);
+    row_kernel<F32, 512, 16, true><<<grid, 512, 0, s>>>(a);
   } else if (pieces <= 16 * 1024) {
-    row_kernel<F32, 1024, 16, GRAD><<<grid, 1024, 0, s>>>(a);
+    row_kernel<F32, 1024, 16, true><<<grid, 1024, 0, s>>>(a);
   } else {
-    row_kernel<F32, 1024, F32 ? 18 : 20, GRAD><<<grid, 1024, 0, s>>>(a);
+    row_kernel<F32, 1024, F32 ? 18 : 20, true><<<grid, 1024, 0, s>>>(a);
   }
   return hipGetLastError();
 }
