@@ -61,14 +61,16 @@ __device__ __forceinline__ void write_once(uint16_t* p, const uint4& v) {
 // form of a held piece across the row's reduction, in twice the registers.
 __device__ __forceinline__ void forget(uint4& p) { asm volatile("" : "+v"(p.x), "+v"(p.y), "+v"(p.z), "+v"(p.w)); }
 
-__device__ __forceinline__ void load_weight(const void* weight, bool f32, int64_t c, float (&w)[8]) {
+// Eight elements of the weight from element first + c on (first: the same in the
+// workgroup).
+__device__ __forceinline__ void load_weight(const void* weight, bool f32, int first, unsigned c, float (&w)[8]) {
   if (f32) {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(weight) + c);
+    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(weight) + first + c);
     const float4 a = p[0], b = p[1];
     w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
     w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
   } else {
-    widen(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(weight) + c), w);
+    widen(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(weight) + first + c), w);
   }
 }
 
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
   for (int i = 0; i < VPT; ++i) {
     const int64_t c = ((int64_t)i * THREADS + t) * 8;
     if (c < a.cols) {
-      load_weight(a.weight, a.weight_f32 != 0, c, w[i]);
+      load_weight(a.weight, a.weight_f32 != 0, i * THREADS * 8, t * 8u, w[i]);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[i][e] = 0.0f;
@@ -222,7 +224,7 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
     if constexpr (kHoldWeight) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) held[i][e] = 0.0f;
-      if (c < a.cols) load_weight(a.weight, a.weight_f32 != 0, c, held[i]);
+      if (c < a.cols) load_weight(a.weight, a.weight_f32 != 0, i * THREADS * 8, t * 8u, held[i]);
     }
   }
   auto weight = [&](int i, float (&w)[8]) {
@@ -233,7 +235,10 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[e] = 0.0f;
-      if (c < a.cols) load_weight(a.weight, a.weight_f32 != 0, c, w);
+      // (loaded again for either pass of a row: kept between them it takes VPT x 8 registers)
+      int first = i * THREADS * 8;
+      asm volatile("" : "+s"(first));
+      if (c < a.cols) load_weight(a.weight, a.weight_f32 != 0, first, t * 8u, w);
     }
   };
   uint4 dy[kNext ? 2 : 1][VPT], h[kNext ? 2 : 1][VPT], dres[kNext ? 2 : 1][VPT];
@@ -268,6 +273,14 @@ __global__ __launch_bounds__(THREADS > kThreads ? THREADS : kThreads) void rmsno
       }
       forget(dy[i]);
       forget(h[i]);
+      if constexpr (!kHoldWeight) {
+        // the sums are formed here: moved past the next pieces' loads they keep the fp32
+        // form of every piece, and rows of more than 16384 elements spill (4096 x 32768
+        // 435 us, so 213)
+        asm volatile("" : "+v"(dot));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(dw[i][e]));
+      }
     }
     const float mean = row_reduce<THREADS, false>(dot, lds[turn]) / (float)a.cols;
 #pragma unroll
