@@ -71,12 +71,13 @@ __device__ __forceinline__ UnitScale unit_scale_fmt(float amax, bool pow2) {
 
 // The same scale without IEEE divisions, for kernels whose every lane forms its
 // units' own: with r = RN(1 / F_max), q = RN(a r) and the exact residual e = a -
-// q F_max, RN(q + e r) is RN32(a / F_max) for every a in the normal range (checked
-// for every mantissa on the CPU); 1 / S is a reciprocal with one Newton step, good
-// to an ulp, which the quotient's own residual step corrects.  Units with a smaller
-// amax (zero among them) take the division, and hand the quotient x and S both
-// times 2^64, exactly, so that every unit's quotients are the same three
-// instructions.
+// q F_max, RN(q + e r) is RN32(a / F_max) for every a in the normal range.  The
+// hardware's reciprocal of S, good to an ulp, is RN32(1 / S) after one Newton step, but for
+// the mantissa of all ones, where the quotient of a power of two alone, no middle
+// between codes, is an ulp off: the quotients' codes are those of RN32(x / S).  (Both are
+// tested on the CPU for every mantissa.)  Units with a smaller amax (zero among them)
+// take the division, and hand the quotient x and S both times 2^64, exactly, so that
+// every unit's quotients are the same three instructions.
 struct CodeScale {
   float s;     // S
   float d, r;  // lift S and its reciprocal
