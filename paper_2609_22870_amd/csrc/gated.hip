@@ -4,9 +4,9 @@
 // sums, in one kernel: the products of gate and up projection never leave the
 // registers unless they are kept for the backward pass.  The kernels are those
 // of gemm_tile.h with a tile of B taken half from each weight.  Bound by the matrix
-// cores and the promotion beside them, as the plain GEMM: 16384 x 4096 x 12288 with
-// quantized output and kept pre-activations 1.55 ms (2.1 PFLOP/s); 8 tokens by the
-// weights, 16 us (6.2 TB/s).
+// cores and the promotion beside it, as the plain GEMM: 16384 x 4096 x 12288 with
+// quantized output and kept pre-activations 1.51 ms (2.2 PFLOP/s); 8 tokens by the
+// weights, 18.2 us with them in memory (5.5 TB/s; 16.3 with them in the last-level cache).
 #include "gemm_tile.h"
 
 namespace fp8q {

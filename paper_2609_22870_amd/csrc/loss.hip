@@ -19,7 +19,8 @@
 // over several workgroups, which leave their sums in a workspace, and a second
 // kernel joins them.  Everything is in base 2 (one fused multiply-add and one
 // v_exp_f32 an element), with the temperature in the factor log2(e) / t.  4096 x
-// 65536 bf16 with the gradient 200 us (5.4 TB/s), 64 x 131072 without 9.6.
+// 65536 bf16 with the gradient 199 us (5.4 TB/s); 64 x 131072 without 11.4 us, its two
+// kernels 8 and 2 of them.
 #include <type_traits>
 
 #include "device_common.h"
@@ -293,7 +294,9 @@ struct Gradient {
     uint8_t* const to = out + head * P::kSize + (int64_t)j0 * 16;
     if (aligned) {
       // past the caches, which keep what is still to be read (4096 x 32000 bf16 108 -> 86
-      // us, 4096 x 65536 fp32 490 -> 425, 8192 x 131072 bf16 853 -> 845)
+      // us, 4096 x 65536 fp32 490 -> 425, 8192 x 131072 bf16 853 -> 845; with the dual
+      // quantizer that reads the gradient next, 128 x 32768 bf16 22.2 -> 20.5, 1024 rows 54.4 ->
+      // 54.7, 4096 x 65536 448 -> 445)
       __builtin_nontemporal_store(v4u{g.x, g.y, g.z, g.w}, reinterpret_cast<v4u*>(to + t * 16u));
     } else {
       const uint32_t w[4] = {g.x, g.y, g.z, g.w};
