@@ -208,11 +208,7 @@ struct Row {
     return p;
   }
   // this thread's single element: its index, or -1
-  __device__ __forceinline__ int edge(int t) const {
-    if (t < head) return t;
-    const int i = head + full * P::kN + (t - 32);
-    return t >= 32 && t < 32 + P::kN && i < V ? i : -1;
-  }
+  __device__ __forceinline__ int edge(int t) const { return row_edge(t, V, head, full, P::kN); }
 };
 
 // What the loss needs of a token besides its logits, and what its row gets.

@@ -101,6 +101,16 @@ struct LossArgs {
 };
 constexpr int kLossParts = 64;  // workgroups that share a row, at most
 constexpr int64_t kLossSplitRows = 128;  // only rows fewer than this are split (see split_rows)
+// The single element of thread t of a row's workgroup, or -1: of a row of V logits whose
+// aligned 16-byte pieces, of n logits each, are `full` from element `head` on, the
+// elements before them are those of threads 0 .., the ones after them those of threads
+// 32 ...  (V is up to 2^31 - 1: no index is formed past it.)
+constexpr int row_edge(int t, int V, int head, int full, int n) {
+  if (t < head) return t;
+  const int end = head + full * n, after = t - 32;
+  return after >= 0 && after < V - end ? end + after : -1;
+}
+
 hipError_t launch_logprobs(const LossArgs& a, hipStream_t s);
 hipError_t launch_policy_loss(const LossArgs& a, hipStream_t s);
 
