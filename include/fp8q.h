@@ -641,6 +641,125 @@ fp8q_status fp8q_policy_loss(const void *logits, fp8q_dtype dtype, int64_t T,
                              int64_t workspace_bytes,
                              struct ihipStream_t *stream);
 
+/*
+ * Four-bit floating point with shared scales (OCP MXFP4), for a rollout's linear
+ * layers: E2M1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) with one scale,
+ * a power of two, per unit of 32 consecutive elements of a row:
+ *   S = 2^(floor(log2 amax) - 2), at least 2^-127, and 1 when amax is 0,
+ *   code = nearest-even E2M1 of x / S, magnitudes above 6 as 6, sign of zero kept.
+ * x / S is exact.  A unit that holds a NaN or an infinity gets the scale byte 255 (NaN):
+ * what is made of it is NaN.  Layout, P being cols rounded up to a multiple of 256:
+ *   codes   bytes [rows][ldc], P / 2 of them a row: element 2 i of a row in the low
+ *           four bits of byte i, element 2 i + 1 in the high ones
+ *   scales  bytes [P / 256][rows][8], S = 2^(byte - 127): the eight units of a row's
+ *           256 elements lie together, those of all its rows one after the other
+ * Elements past cols are zeros; units of them have the byte 127.
+ *
+ * fp8q_quantize_mx4: x bf16 [rows][ldx], any cols and ldx >= cols, ldc >= P / 2.
+ * Alignment: x 2-byte (16-byte with ldx % 8 == 0 reads faster), codes 16-byte, ldc % 16
+ * == 0, scales 8-byte aligned (else FP8Q_ERR_ALIGN).  Up to 2^23 tiles of 32 x 512
+ * elements (else FP8Q_ERR_UNSUPPORTED).
+ */
+fp8q_status fp8q_quantize_mx4(const void *x, int64_t rows, int64_t cols,
+                              int64_t ldx, uint8_t *codes, int64_t ldc,
+                              uint8_t *scales, struct ihipStream_t *stream);
+
+/*
+ * The values of MXFP4 codes, y bf16 [rows][ldy]: the first cols elements of each row
+ * (exact, but past bf16's range infinite).  codes, scales and their alignment as
+ * fp8q_quantize_mx4 has them; y 2-byte aligned, any ldy >= cols.
+ */
+fp8q_status fp8q_dequantize_mx4(const uint8_t *codes, int64_t ldc,
+                                const uint8_t *scales, int64_t rows,
+                                int64_t cols, void *y, int64_t ldy,
+                                struct ihipStream_t *stream);
+
+/*
+ * C[m][n] = sum_k A[m][k] B[n][k] of the values of MXFP4 operands, fp32 accumulation,
+ * bf16 round-to-nearest-even output: Y = X W^T of a linear layer, both operands from
+ * fp8q_quantize_mx4.
+ *   A, sA  codes [M][lda] and scales of M rows of K elements; B, sB of N rows
+ *   C      bf16 [M][ldc]
+ * K counts codes, zeros past a row's end among them: a multiple of 256; M and N are free.
+ * lda, ldb in bytes, at least K / 2.  M K / 32 and N K / 32 below 2^31 (else
+ * FP8Q_ERR_UNSUPPORTED).  Alignment: A and B 16-byte aligned, lda % 16 == 0, ldb % 16 == 0;
+ * sA and sB 8-byte aligned; C 8-byte aligned with ldc % 4 == 0.  Results are the same on
+ * every run.
+ */
+fp8q_status fp8q_gemm_mx4(const uint8_t *A, const uint8_t *sA, int64_t lda,
+                          const uint8_t *B, const uint8_t *sB, int64_t ldb,
+                          int64_t M, int64_t N, int64_t K, void *C, int64_t ldc,
+                          struct ihipStream_t *stream);
+
+/*
+ * Rows of an embedding table for T tokens: y[t] = scale weight[token], bf16 [T][ldy],
+ * rounded once from fp32; weight [V][ldw], bf16 or fp32 (dtype).  A token outside
+ * 0 .. V-1 (padding) gives a row of zeros.  Shape rules: C % 16 == 0, T below 2^22
+ * (else FP8Q_ERR_UNSUPPORTED).  Alignment: weight and y 16-byte aligned, ldy % 8 == 0, ldw % 8
+ * == 0 (fp32: % 4); tokens 8-byte.  scale finite (else FP8Q_ERR_INVAL).
+ */
+fp8q_status fp8q_embedding(const void *weight, fp8q_dtype dtype, int64_t V,
+                           int64_t C, int64_t ldw, const int64_t *tokens,
+                           int64_t T, double scale, void *y, int64_t ldy,
+                           struct ihipStream_t *stream);
+
+/*
+ * Bytes of workspace fp8q_embedding_backward needs; -1 for a size it refuses.
+ */
+int64_t fp8q_embedding_backward_workspace(int64_t T, int64_t V, int64_t C);
+
+/* dweight holds a gradient already, which the call adds to. */
+enum { FP8Q_ACCUMULATE = 32u };
+
+/*
+ * The table's gradient from that of y (dy bf16 [T][lddy]): dweight[v] = scale times the
+ * sum of dy[t] over the tokens t that are v, [V][ldw] in dtype, summed in fp32 in one order
+ * that depends on T and the tokens alone (the results are the same on every run) and rounded
+ * once.  Rows of tokens that do not occur are zero; with FP8Q_ACCUMULATE (flags) they are
+ * not touched, and the others get the sum added in fp32 to what they hold.  Tokens outside
+ * 0 .. V-1 take no part (their rows of dy are not read).
+ * workspace: at least fp8q_embedding_backward_workspace(T, V, C) bytes, 16-byte aligned,
+ * overwritten (calls that share one must be ordered).  Shape rules: C % 16 == 0, T below 2^22,
+ * V C below 2^40 (else FP8Q_ERR_UNSUPPORTED).  Alignment: as fp8q_embedding.  dweight must not
+ * overlap dy.
+ */
+fp8q_status fp8q_embedding_backward(const void *dy, int64_t lddy,
+                                    const int64_t *tokens, int64_t T, int64_t V,
+                                    int64_t C, double scale, unsigned flags,
+                                    void *dweight, fp8q_dtype dtype,
+                                    int64_t ldw, void *workspace,
+                                    int64_t workspace_bytes,
+                                    struct ihipStream_t *stream);
+
+/* Alternatives of a row of fp8q_top_logprobs, at most. */
+enum { FP8Q_MAX_TOP = 64 };
+
+/*
+ * Bytes of workspace fp8q_top_logprobs needs (0 for sizes that need none); -1 for a size
+ * it refuses.
+ */
+int64_t fp8q_top_logprobs_workspace(int64_t T, int64_t V, int64_t k);
+
+/*
+ * fp8q_token_logprobs with the k most probable alternatives of every row, from one read of
+ * the logits:
+ *   ids   int64 [T][k]: the indices of the k largest logits, in descending order, of
+ *         equal ones (-0 is 0) the lower index first
+ *   top   fp32 [T][k]: their log-probabilities
+ * A logit of -inf (or NaN) is no alternative: with fewer than k others the places left over
+ * hold -1 and -inf.  A row whose token is outside the vocabulary is not read: its logp,
+ * entropy and top are 0 and its ids -1.  k in 1 .. FP8Q_MAX_TOP and at most V (else
+ * FP8Q_ERR_INVAL).  Otherwise the rules of fp8q_token_logprobs; ids 8-byte, top 4-byte
+ * aligned.  workspace: at least fp8q_top_logprobs_workspace(T, V, k) bytes, 16-byte aligned
+ * (null where that is 0), overwritten (calls that share one must be ordered).
+ */
+fp8q_status fp8q_top_logprobs(const void *logits, fp8q_dtype dtype, int64_t T,
+                              int64_t V, int64_t ld, const int64_t *tokens,
+                              int64_t k, double temperature, float *logp,
+                              float *entropy, int64_t *ids, float *top,
+                              void *workspace, int64_t workspace_bytes,
+                              struct ihipStream_t *stream);
+
 /* Static string naming a status. */
 const char *fp8q_status_string(fp8q_status status);
 

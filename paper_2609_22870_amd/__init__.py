@@ -25,6 +25,8 @@ LIB_PATH = os.path.join(_HERE, "libfp8q.so")
 TENSOR, ROW, COL, BLOCK_1x128, BLOCK_128x1, BLOCK_128x128 = range(6)
 OUT_TRANSPOSED = 1
 POW2_SCALE = 2
+ACCUMULATE = 32               # embedding_backward flag: dweight is added to
+MAX_TOP = 64                  # alternatives of top_logprobs, at most
 E5M2 = 4                      # quantize flag: E5M2 codes (F_max = 57344)
 WEIGHT_F32 = 16               # norm flag: its weight is fp32
 A_E5M2, B_E5M2 = 1, 2         # gemm_formats operand formats
@@ -40,7 +42,9 @@ EXPORTS = ("fp8q_scales_count", "fp8q_quantize", "fp8q_quantize_dual",
            "fp8q_rmsnorm_backward", "fp8q_gemm_gated", "fp8q_gemm_gated_workspace", "fp8q_gemm_gated_quantized",
            "fp8q_gated_backward",
            "fp8q_requantize_transposed", "fp8q_policy_loss_workspace", "fp8q_token_logprobs", "fp8q_policy_loss",
-           "fp8q_status_string")
+           "fp8q_quantize_mx4", "fp8q_dequantize_mx4", "fp8q_gemm_mx4", "fp8q_embedding",
+           "fp8q_embedding_backward_workspace", "fp8q_embedding_backward", "fp8q_top_logprobs_workspace",
+           "fp8q_top_logprobs", "fp8q_status_string")
 
 
 MAX_GROUP = 8
@@ -98,7 +102,9 @@ _NATIVE_API = ("fp8q_scales_count", "fp8q_quantize", "fp8q_quantize_dual", "fp8q
                "fp8q_rmsnorm_backward_workspace", "fp8q_rmsnorm_backward", "fp8q_gemm_gated",
                "fp8q_gemm_gated_workspace", "fp8q_gemm_gated_quantized", "fp8q_gated_backward",
                "fp8q_requantize_transposed",
-               "fp8q_policy_loss_workspace", "fp8q_token_logprobs", "fp8q_policy_loss")
+               "fp8q_policy_loss_workspace", "fp8q_token_logprobs", "fp8q_policy_loss", "fp8q_quantize_mx4",
+               "fp8q_dequantize_mx4", "fp8q_gemm_mx4", "fp8q_embedding", "fp8q_embedding_backward_workspace",
+               "fp8q_embedding_backward", "fp8q_top_logprobs_workspace", "fp8q_top_logprobs")
 
 
 def lib():
@@ -171,6 +177,22 @@ def lib():
         L.fp8q_token_logprobs.restype = i32
         L.fp8q_policy_loss.argtypes = [p, i32, i64, i64, i64, ctypes.POINTER(PolicyBatch), p, p, i64, p, p, p, i64, p]
         L.fp8q_policy_loss.restype = i32
+        L.fp8q_quantize_mx4.argtypes = [p, i64, i64, i64, p, i64, p, p]
+        L.fp8q_quantize_mx4.restype = i32
+        L.fp8q_dequantize_mx4.argtypes = [p, i64, p, i64, i64, p, i64, p]
+        L.fp8q_dequantize_mx4.restype = i32
+        L.fp8q_gemm_mx4.argtypes = [p, p, i64, p, p, i64, i64, i64, i64, p, i64, p]
+        L.fp8q_gemm_mx4.restype = i32
+        L.fp8q_embedding.argtypes = [p, i32, i64, i64, i64, p, i64, d, p, i64, p]
+        L.fp8q_embedding.restype = i32
+        L.fp8q_embedding_backward_workspace.argtypes = [i64, i64, i64]
+        L.fp8q_embedding_backward_workspace.restype = i64
+        L.fp8q_embedding_backward.argtypes = [p, i64, p, i64, i64, i64, d, u32, p, i32, i64, p, i64, p]
+        L.fp8q_embedding_backward.restype = i32
+        L.fp8q_top_logprobs_workspace.argtypes = [i64, i64, i64]
+        L.fp8q_top_logprobs_workspace.restype = i64
+        L.fp8q_top_logprobs.argtypes = [p, i32, i64, i64, i64, p, i64, d, p, p, p, p, p, i64, p]
+        L.fp8q_top_logprobs.restype = i32
         L.fp8q_status_string.argtypes = [i32]
         L.fp8q_status_string.restype = ctypes.c_char_p
         native.bind(tuple(ctypes.cast(getattr(L, n), p).value for n in _NATIVE_API))
@@ -815,3 +837,166 @@ def policy_loss(logits, tokens, logp_old, adv, weight, clip_low, clip_high, beta
                                 workspace.data_ptr(), workspace.numel(), _stream(logits))
     _check(st, "fp8q_policy_loss")
     return loss, dlogits, logp, entropy
+
+
+def _mx4_row_bytes(cols):
+    """Bytes of MXFP4 codes of a row of cols elements (its length rounded up to a multiple of 256)."""
+    return (cols + 255) // 256 * 128
+
+
+def _mx4(codes, scales, what, device=None):
+    """MXFP4 operands checked: codes [rows, K / 2] and the scales of their rows; returns rows, K."""
+    _matrix(codes, torch.uint8, what, device=device)
+    rows, row_bytes = codes.shape
+    if row_bytes % 128:
+        raise ValueError("%s must have whole pieces of 256 codes in a row" % what)
+    _vector(scales, torch.uint8, rows * (row_bytes // 16), "scales of %s" % what, codes.device)
+    return rows, row_bytes * 2
+
+
+def quantize_mx4(x, codes=None, scales=None):
+    """MXFP4 (E2M1 codes, a power-of-two scale per 32 elements of a row) of a bf16 CUDA
+    tensor x[rows, cols]: returns (codes, scales), an operand of gemm_mx4().  With P =
+    cols rounded up to a multiple of 256: codes uint8 [rows, P / 2], two a byte, the first in
+    the low half, zeros past cols; scales uint8 [rows * P / 32], exponent + 127, laid out
+    [P / 256][rows][8] (see fp8q_quantize_mx4)."""
+    r = _fast().quantize_mx4(x, codes, scales)
+    if r is not None:
+        return _done(r, "fp8q_quantize_mx4")
+    _matrix(x, torch.bfloat16, "x")
+    rows, cols = x.shape
+    codes = _given(codes, torch.uint8, "codes", (rows, _mx4_row_bytes(cols)), x.device)
+    scales = _new_vector(scales, torch.uint8, rows * (_mx4_row_bytes(cols) // 16), "scales", x.device)
+    st = lib().fp8q_quantize_mx4(x.data_ptr(), rows, cols, _ld(x), codes.data_ptr(), _ld(codes), scales.data_ptr(),
+                                 _stream(x))
+    _check(st, "fp8q_quantize_mx4")
+    return codes, scales
+
+
+def dequantize_mx4(codes, scales, cols=None, out=None):
+    """The values of MXFP4 codes as quantize_mx4() gives them, bf16 [rows, cols]: the first
+    `cols` elements of each row (all of them, with the zeros that fill it up, when None)."""
+    if cols is None and isinstance(codes, torch.Tensor) and codes.dim() == 2:
+        cols = codes.shape[1] * 2
+    r = _fast().dequantize_mx4(codes, scales, cols, out)
+    if r is not None:
+        return _done(r, "fp8q_dequantize_mx4")
+    rows, K = _mx4(codes, scales, "codes")
+    if not 1 <= cols <= K:
+        raise ValueError("cols must lie in 1 .. %d" % K)
+    out = _given(out, torch.bfloat16, "out", (rows, cols), codes.device)
+    st = lib().fp8q_dequantize_mx4(codes.data_ptr(), _ld(codes), scales.data_ptr(), rows, cols, out.data_ptr(), _ld(out),
+                                   _stream(codes))
+    _check(st, "fp8q_dequantize_mx4")
+    return out
+
+
+def gemm_mx4(a, sa, b, sb, out=None):
+    """bf16 out[M, N] = A B^T of MXFP4 operands as quantize_mx4() gives them: a, sa the codes
+    [M, K / 2] and scales of the activations, b, sb those of a weight stored [N, K]; fp32
+    accumulation."""
+    r = _fast().gemm_mx4(a, sa, b, sb, out)
+    if r is not None:
+        return _done(r, "fp8q_gemm_mx4")
+    M, K = _mx4(a, sa, "a")
+    N, K2 = _mx4(b, sb, "b", a.device)
+    if K != K2:
+        raise ValueError("contraction sizes differ")
+    out = _given(out, torch.bfloat16, "out", (M, N), a.device)
+    st = lib().fp8q_gemm_mx4(a.data_ptr(), sa.data_ptr(), _ld(a), b.data_ptr(), sb.data_ptr(), _ld(b), M, N, K,
+                             out.data_ptr(), _ld(out), _stream(a))
+    _check(st, "fp8q_gemm_mx4")
+    return out
+
+
+def _tokens(tokens, device, T=None):
+    """tokens checked: int64 [T] on the device; returns T."""
+    _vector(tokens, torch.int64, 0, "tokens", device)
+    if tokens.dim() != 1 or (T is not None and tokens.numel() != T):
+        raise ValueError("tokens must be a vector of one token a row")
+    return tokens.numel()
+
+
+def embedding(weight, tokens, scale=1.0, out=None):
+    """Rows of an embedding table, scaled: bf16 out[T, C] = scale weight[tokens], weight
+    bf16 or fp32 [V, C], tokens int64 [T].  A token outside the table (padding) gives a row
+    of zeros."""
+    r = _fast().embedding(weight, tokens, scale, out)
+    if r is not None:
+        return _done(r, "fp8q_embedding")
+    if not isinstance(weight, torch.Tensor) or weight.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("weight must be a 2-D bfloat16 or float32 CUDA tensor")
+    _matrix(weight, weight.dtype, "weight")
+    T = _tokens(tokens, weight.device)
+    V, C = weight.shape
+    out = _given(out, torch.bfloat16, "out", (T, C), weight.device)
+    st = lib().fp8q_embedding(weight.data_ptr(), 1 if weight.dtype == torch.float32 else 0, V, C, _ld(weight),
+                              tokens.data_ptr(), T, float(scale), out.data_ptr(), _ld(out), _stream(weight))
+    _check(st, "fp8q_embedding")
+    return out
+
+
+def embedding_backward(dy, tokens, vocab, scale=1.0, dtype=torch.float32, dweight=None, accumulate=False,
+                       workspace=None):
+    """Gradient of embedding()'s table from that of its output, dy bf16 [T, C]: dweight
+    [vocab, C] in `dtype` (float32 or bfloat16), each row the sum of its tokens' rows of dy
+    in fp32, times scale, in one order (the same bits on every run); rows of tokens that do
+    not occur are zero.  accumulate: dweight (given) is added to, and rows of tokens that do not
+    occur stay as they are.  workspace: a uint8 CUDA tensor of
+    fp8q_embedding_backward_workspace bytes (a new one when None)."""
+    r = _fast().embedding_backward(dy, tokens, vocab, scale, dtype is torch.float32, dweight, accumulate,
+                                   workspace) if dtype in (torch.float32, torch.bfloat16) else None
+    if r is not None:
+        return _done(r, "fp8q_embedding_backward")
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dtype must be float32 or bfloat16")
+    _matrix(dy, torch.bfloat16, "dy")
+    T, C = dy.shape
+    _tokens(tokens, dy.device, T)
+    if accumulate and dweight is None:
+        raise ValueError("accumulate needs the dweight that is added to")
+    need = lib().fp8q_embedding_backward_workspace(T, vocab, C)
+    if need < 0:
+        raise ValueError("invalid number of tokens, vocabulary size or width")
+    dweight = _given(dweight, dtype, "dweight", (vocab, C), dy.device)
+    workspace = _new_vector(workspace, torch.uint8, need, "workspace", dy.device)
+    st = lib().fp8q_embedding_backward(dy.data_ptr(), _ld(dy), tokens.data_ptr(), T, vocab, C, float(scale),
+                                       ACCUMULATE if accumulate else 0, dweight.data_ptr(),
+                                       1 if dtype is torch.float32 else 0, _ld(dweight), workspace.data_ptr(),
+                                       workspace.numel(), _stream(dy))
+    _check(st, "fp8q_embedding_backward")
+    return dweight
+
+
+def top_logprobs(logits, tokens, k, temperature=1.0, logp=None, entropy=None, ids=None, top=None, workspace=None):
+    """token_logprobs() with each row's k most probable alternatives (k up to MAX_TOP), from one
+    read of the logits: returns (logp, entropy, ids, top), ids int64 [T, k] the indices of the
+    k largest logits in descending order, equal ones by index, top fp32 [T, k] their
+    log-probabilities.  A logit of -inf is no alternative: places left over hold -1 and -inf.  A
+    token outside the vocabulary gives 0, 0, ids of -1 and a top of 0.  workspace: a uint8 CUDA
+    tensor of fp8q_top_logprobs_workspace bytes (a new one when None and the size needs one)."""
+    r = _fast().top_logprobs(logits, tokens, k, temperature, logp, entropy, ids, top, workspace)
+    if r is not None:
+        return _done(r, "fp8q_top_logprobs")
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("logits must be a 2-D bfloat16 or float32 CUDA tensor")
+    _matrix(logits, logits.dtype, "logits")
+    T, V = logits.shape
+    dev = logits.device
+    _vector(tokens, torch.int64, T, "tokens", dev)
+    need = lib().fp8q_top_logprobs_workspace(T, V, k)
+    if need < 0:
+        raise ValueError("invalid number of tokens, vocabulary size or k")
+    logp = _new_vector(logp, torch.float32, T, "logp", dev)
+    entropy = _new_vector(entropy, torch.float32, T, "entropy", dev)
+    ids = _given(ids, torch.int64, "ids", (T, k), dev)
+    top = _given(top, torch.float32, "top", (T, k), dev)
+    if not ids.is_contiguous() or not top.is_contiguous():
+        raise ValueError("ids and top must be contiguous")
+    workspace = _new_vector(workspace, torch.uint8, need, "workspace", dev)
+    st = lib().fp8q_top_logprobs(logits.data_ptr(), 1 if logits.dtype == torch.float32 else 0, T, V, _ld(logits),
+                                 tokens.data_ptr(), k, float(temperature), logp.data_ptr(), entropy.data_ptr(),
+                                 ids.data_ptr(), top.data_ptr(), workspace.data_ptr() if need else None,
+                                 workspace.numel(), _stream(logits))
+    _check(st, "fp8q_top_logprobs")
+    return logp, entropy, ids, top

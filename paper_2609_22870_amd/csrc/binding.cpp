@@ -57,6 +57,14 @@ struct Api {
   decltype(&fp8q_policy_loss_workspace) loss_workspace;
   decltype(&fp8q_token_logprobs) token_logprobs;
   decltype(&fp8q_policy_loss) policy_loss;
+  decltype(&fp8q_quantize_mx4) quantize_mx4;
+  decltype(&fp8q_dequantize_mx4) dequantize_mx4;
+  decltype(&fp8q_gemm_mx4) gemm_mx4;
+  decltype(&fp8q_embedding) embedding;
+  decltype(&fp8q_embedding_backward_workspace) embedding_workspace;
+  decltype(&fp8q_embedding_backward) embedding_backward;
+  decltype(&fp8q_top_logprobs_workspace) top_workspace;
+  decltype(&fp8q_top_logprobs) top_logprobs;
 };
 constexpr Py_ssize_t kApiSize = sizeof(Api) / sizeof(void*);
 
@@ -739,6 +747,169 @@ PyObject* py_policy_loss(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Bytes of MXFP4 codes that a row of cols elements takes, and of its scales.
+int64_t mx4_row_bytes(int64_t cols) { return (cols + 255) / 256 * 128; }
+
+// MXFP4 operands: codes [rows, K / 2] with the scales of their rows.
+struct Mx4 {
+  const uint8_t *codes, *scales;
+  int64_t rows, K, ld;
+  Mx4(PyObject* oc, PyObject* os, c10::Device device) {
+    const at::Tensor& c = matrix(oc, at::kByte);
+    if (c.device() != device || c.size(1) % 128) leave();
+    rows = c.size(0);
+    K = c.size(1) * 2;
+    ld = c.stride(0);
+    codes = c.const_data_ptr<uint8_t>();
+    scales = vector(os, at::kByte, rows * (K / 32), device).const_data_ptr<uint8_t>();
+  }
+};
+
+// quantize_mx4(x, codes, scales) -> (codes, scales)
+PyObject* py_quantize_mx4(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<3>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const at::Tensor& x = matrix(a[0], at::kBFloat16);
+    const int64_t rows = x.size(0), cols = x.size(1), bytes = mx4_row_bytes(cols);
+    const at::Tensor codes = matrix_or_new(a[1], at::kByte, rows, bytes, x.device());
+    const at::Tensor scales = vector_or_new(a[2], at::kByte, rows * (bytes / 16), x.device());
+    const void* xp = x.const_data_ptr();
+    uint8_t *cp = codes.mutable_data_ptr<uint8_t>(), *sp = scales.mutable_data_ptr<uint8_t>();
+    ihipStream_t* s = stream_of(x);
+    const fp8q_status st = unlocked([&] {
+      return api.quantize_mx4(xp, rows, cols, x.stride(0), cp, codes.stride(0), sp, s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[1], codes), give(a[2], scales)});
+  });
+}
+
+// dequantize_mx4(codes, scales, cols, out) -> out
+PyObject* py_dequantize_mx4(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<4>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const c10::Device device = tensor(a[0]).device();
+    const Mx4 q(a[0], a[1], device);
+    const int64_t cols = integer(a[2]);
+    if (cols < 1 || cols > q.K) leave();
+    const at::Tensor out = matrix_or_new(a[3], at::kBFloat16, q.rows, cols, device);
+    void* yp = out.mutable_data_ptr();
+    ihipStream_t* s = stream_of(out);
+    const fp8q_status st = unlocked([&] {
+      return api.dequantize_mx4(q.codes, q.ld, q.scales, q.rows, cols, yp, out.stride(0), s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return give(a[3], out);
+  });
+}
+
+// gemm_mx4(a, sa, b, sb, out) -> out
+PyObject* py_gemm_mx4(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<5>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const c10::Device device = tensor(a[0]).device();
+    const Mx4 p(a[0], a[1], device), q(a[2], a[3], device);
+    if (p.K != q.K) leave();
+    const at::Tensor out = matrix_or_new(a[4], at::kBFloat16, p.rows, q.rows, device);
+    void* cp = out.mutable_data_ptr();
+    ihipStream_t* s = stream_of(out);
+    const fp8q_status st = unlocked([&] {
+      return api.gemm_mx4(p.codes, p.scales, p.ld, q.codes, q.scales, q.ld, p.rows, q.rows, p.K, cp, out.stride(0), s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return give(a[4], out);
+  });
+}
+
+// embedding(weight, tokens, scale, out) -> out
+PyObject* py_embedding(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<4>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const fp8q_dtype dtype = tensor(a[0]).scalar_type() == at::kFloat ? FP8Q_F32 : FP8Q_BF16;
+    const at::Tensor& w = matrix(a[0], dtype == FP8Q_F32 ? at::kFloat : at::kBFloat16);
+    const at::Tensor& tokens = vector(a[1], at::kLong, 0, w.device());
+    if (tokens.dim() != 1) leave();
+    const double scale = real(a[2]);
+    const int64_t T = tokens.size(0), V = w.size(0), C = w.size(1);
+    const at::Tensor out = matrix_or_new(a[3], at::kBFloat16, T, C, w.device());
+    const void* wp = w.const_data_ptr();
+    const int64_t* tp = tokens.const_data_ptr<int64_t>();
+    void* yp = out.mutable_data_ptr();
+    ihipStream_t* s = stream_of(w);
+    const fp8q_status st = unlocked([&] {
+      return api.embedding(wp, dtype, V, C, w.stride(0), tp, T, scale, yp, out.stride(0), s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return give(a[3], out);
+  });
+}
+
+// embedding_backward(dy, tokens, vocab, scale, f32, dweight, accumulate, workspace) -> dweight
+PyObject* py_embedding_backward(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<8>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const at::Tensor& dy = matrix(a[0], at::kBFloat16);
+    const c10::Device device = dy.device();
+    const at::Tensor& tokens = vector(a[1], at::kLong, 0, device);
+    const int64_t T = dy.size(0), C = dy.size(1), V = integer(a[2]);
+    if (tokens.dim() != 1 || tokens.size(0) != T) leave();
+    const double scale = real(a[3]);
+    const bool f32 = truth(a[4]), accumulate = truth(a[6]);
+    if (accumulate && a[5] == Py_None) leave();
+    const int64_t need = api.embedding_workspace(T, V, C);
+    if (need < 0) leave();
+    const at::Tensor dw = matrix_or_new(a[5], f32 ? at::kFloat : at::kBFloat16, V, C, device);
+    const at::Tensor ws = vector_or_new(a[7], at::kByte, need, device);
+    const void* dyp = dy.const_data_ptr();
+    const int64_t* tp = tokens.const_data_ptr<int64_t>();
+    void *dwp = dw.mutable_data_ptr(), *wp = ws.mutable_data_ptr();
+    const int64_t bytes = ws.numel();
+    ihipStream_t* s = stream_of(dy);
+    const fp8q_status st = unlocked([&] {
+      return api.embedding_backward(dyp, dy.stride(0), tp, T, V, C, scale, accumulate ? FP8Q_ACCUMULATE : 0u, dwp,
+                                    f32 ? FP8Q_F32 : FP8Q_BF16, dw.stride(0), wp, bytes, s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return give(a[5], dw);
+  });
+}
+
+// top_logprobs(logits, tokens, k, temperature, logp, entropy, ids, top, workspace) -> (logp,
+// entropy, ids, top)
+PyObject* py_top_logprobs(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return guarded<9>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
+    const fp8q_dtype dtype = tensor(a[0]).scalar_type() == at::kFloat ? FP8Q_F32 : FP8Q_BF16;
+    const at::Tensor& x = matrix(a[0], dtype == FP8Q_F32 ? at::kFloat : at::kBFloat16);
+    const c10::Device device = x.device();
+    const int64_t T = x.size(0), V = x.size(1), k = integer(a[2]);
+    const int64_t* tokens = vector(a[1], at::kLong, T, device).const_data_ptr<int64_t>();
+    const double temperature = real(a[3]);
+    const int64_t need = api.top_workspace(T, V, k);
+    if (need < 0) leave();
+    const at::Tensor logp = vector_or_new(a[4], at::kFloat, T, device);
+    const at::Tensor entropy = vector_or_new(a[5], at::kFloat, T, device);
+    auto contiguous = [&](PyObject* o, at::ScalarType type) {
+      const at::Tensor t = matrix_or_new(o, type, T, k, device);
+      if (!t.is_contiguous()) leave();
+      return t;
+    };
+    const at::Tensor ids = contiguous(a[6], at::kLong), top = contiguous(a[7], at::kFloat);
+    at::Tensor ws;
+    void* wp = nullptr;
+    int64_t bytes = 0;
+    if (need > 0) {
+      ws = vector_or_new(a[8], at::kByte, need, device);
+      wp = ws.mutable_data_ptr();
+      bytes = ws.numel();
+    }
+    const void* xp = x.const_data_ptr();
+    float *lp = logp.mutable_data_ptr<float>(), *ep = entropy.mutable_data_ptr<float>();
+    int64_t* ip = ids.mutable_data_ptr<int64_t>();
+    float* kp = top.mutable_data_ptr<float>();
+    ihipStream_t* s = stream_of(x);
+    const fp8q_status st = unlocked([&] {
+      return api.top_logprobs(xp, dtype, T, V, x.stride(0), tokens, k, temperature, lp, ep, ip, kp, wp, bytes, s);
+    });
+    if (st != FP8Q_OK) return PyLong_FromLong(st);
+    return pack({give(a[4], logp), give(a[5], entropy), give(a[6], ids), give(a[7], top)});
+  });
+}
+
 // bind((address, ..)): the entry points of Api, in its order
 PyObject* py_bind(PyObject* m, PyObject* addresses) {
   if (!PyTuple_CheckExact(addresses) || PyTuple_GET_SIZE(addresses) != kApiSize) {
@@ -777,6 +948,12 @@ PyMethodDef methods[] = {
     {"requantize_transposed", FAST(py_requantize_transposed), nullptr},
     {"token_logprobs", FAST(py_token_logprobs), nullptr},
     {"policy_loss", FAST(py_policy_loss), nullptr},
+    {"quantize_mx4", FAST(py_quantize_mx4), nullptr},
+    {"dequantize_mx4", FAST(py_dequantize_mx4), nullptr},
+    {"gemm_mx4", FAST(py_gemm_mx4), nullptr},
+    {"embedding", FAST(py_embedding), nullptr},
+    {"embedding_backward", FAST(py_embedding_backward), nullptr},
+    {"top_logprobs", FAST(py_top_logprobs), nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, sizeof(Api), methods, nullptr, nullptr, nullptr, nullptr};

@@ -40,6 +40,7 @@ namespace fp8q {
 namespace gemm_detail {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned int v4u __attribute__((ext_vector_type(4)));
 typedef unsigned int v2u __attribute__((ext_vector_type(2)));
@@ -66,6 +67,21 @@ __device__ __forceinline__ v4f mfma_16x16x128(const v8i& a, const v8i& b, const 
 __device__ __forceinline__ v4f mfma_16x16x128_e8(const v8i& a, const v8i& b, const v4f& c, int scale_a,
                                                  int scale_b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
+}
+
+// The same for E2M1 codes (cbsz, blgp 4): a lane holds 32 codes of its row, 16 bytes, in
+// the first four registers of `a` and `b`.  H: the byte of scale_a and scale_b that the
+// instruction takes.  It runs in half the time of the FP8 one.
+template <int H>
+__device__ __forceinline__ v4f mfma_16x16x128_mx4(const v4i& a, const v4i& b, const v4f& c, int scale_a, int scale_b) {
+  const v8i wa = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, wb = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, wb, c, 4, 4, H, scale_a, H, scale_b);
+}
+
+// Half H of a fragment read as for FP8: the 16 bytes of one of its two chunks.
+template <int H>
+__device__ __forceinline__ v4i half_frag(const v8i& f) {
+  return v4i{f[4 * H], f[4 * H + 1], f[4 * H + 2], f[4 * H + 3]};
 }
 
 // E8M0 byte of a power-of-two fp32 scale in [2^-127, 2^127]: its exponent
@@ -216,6 +232,11 @@ __device__ __forceinline__ float lds_read_f32(uint32_t addr, int imm) {
   asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(imm));
   return v;
 }
+__device__ __forceinline__ int lds_read_u16(uint32_t addr, int imm) {
+  int v;
+  asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(imm));
+  return v;
+}
 __device__ __forceinline__ void lds_read_f32x4(uint32_t addr, float (&v)[4]) {
   float4 t;
   asm volatile("ds_read_b128 %0, %1" : "=v"(t) : "v"(addr));
@@ -224,6 +245,7 @@ __device__ __forceinline__ void lds_read_f32x4(uint32_t addr, float (&v)[4]) {
 
 // After an LDS wait that covers v's read: v counts as written here.
 __device__ __forceinline__ void lds_arrived(float& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void lds_arrived(int& v) { asm volatile("" : "+v"(v)); }
 
 // Wait until at most N LDS reads of this wave are outstanding, and make
 // `f` (whose reads were issued before the last N) count as written here.
@@ -547,15 +569,17 @@ __device__ __forceinline__ void gated_epilogue(const GatedArgs& g, const v4f (&a
 // their scale vectors, and 256 bytes per wave (see gemm_tile).
 template <int PAIR, int BM, int BN, int WM, int WN, int KS = 1>
 struct TileLds {
-  static constexpr bool kBlockScaled = PAIR == kPairBlock || PAIR == kPairBlockK || PAIR == kPairBlockE8;
+  static constexpr bool kMx = PAIR == kPairMx4;
+  static constexpr bool kBlockScaled = PAIR == kPairBlock || PAIR == kPairBlockK || PAIR == kPairBlockE8 || kMx;
   static constexpr bool kWeightBlocks = PAIR == kPairBlock || PAIR == kPairBlockE8;  // B scales per 128 x 128
   static constexpr int kWaves = (BM / WM) * (BN / WN);
   static constexpr int kStage = (BM + BN) * kBK;
   // per-step scale vectors of the blockwise pairs, staged like the tiles:
   // A row scales (BM floats) and B scales (the BN/128 weight-block scales,
-  // or BN column scales for 1x128 x 1x128)
-  static constexpr int kScaleA = kBlockScaled ? BM * 4 : 0;
-  static constexpr int kScaleB = PAIR == kPairBlockK ? BN * 4 : (kWeightBlocks ? 256 : 0);
+  // or BN column scales for 1x128 x 1x128); with E2M1 codes the eight scale
+  // bytes of each row
+  static constexpr int kScaleA = kMx ? BM * 8 : (kBlockScaled ? BM * 4 : 0);
+  static constexpr int kScaleB = kMx ? BN * 8 : (PAIR == kPairBlockK ? BN * 4 : (kWeightBlocks ? 256 : 0));
   // The loads of stage kt + kStages - 1 go out during step kt.  The 256 x
   // 256 tile fits two 64 KB stages; 128 x 256 and 128 x 128 with waves of 64
   // x 64 keep two (more would cost the latter its second workgroup per CU);
@@ -697,14 +721,41 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
     q_ld = uniform(q_ld);
     q_base = uniform(q_base);
   };
-  scale_offsets();
+  if constexpr (!Lds::kMx) scale_offsets();
   // LDS destination of this wave's instruction: stage st's scale vectors
   uint8_t* const q_to = wave < kQ ? scale_lds + q_dst : dummy_lds + wave_all * 256;
   const int q_stride = uniform(wave < kQ ? kScaleStage : 0);
-  auto load_scales = [&](int kt, int st) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_q, (lds_void*)(q_to + st * q_stride), 4, q_voff,
-                                             q_base + kt * q_ld, 0, 0);
+  // E2M1: the scale bytes of 32 rows an instruction, in kMxLoads of them a wave; wave w
+  // issues instructions w, w + kWaves, ... of A's and then B's (those past them, as above,
+  // load nothing into the dummy corner)
+  constexpr int kMxLoads = Lds::kMx ? (kQ + kWaves - 1) / kWaves : 1;
+  int x_voff[kMxLoads], x_base[kMxLoads], x_ld[kMxLoads], x_to[kMxLoads], x_stride[kMxLoads];
+  if constexpr (Lds::kMx) {
+    const int last_m = (int)(g.M - 1 - m0), last_n = (int)(g.N - 1 - n0);
+    static_for<kMxLoads>([&](auto sc) {
+      constexpr int s = decltype(sc)::value;
+      const int q = wave + s * kWaves;
+      const bool is_a = q < kQA, live = q < kQ;
+      const int r = (is_a ? q : q - kQA) * 32 + (lane >> 1), last = is_a ? last_m : last_n;
+      x_voff[s] = live ? (r < last ? r : last) * 8 + (lane & 1) * 4 : 0x7fffffff;
+      x_base[s] = uniform((int)(is_a ? m0 : n0) * 8);
+      x_ld[s] = uniform((int)(is_a ? g.sa_ld : g.sb_ld) * 4);
+      x_to[s] = uniform((int)((live ? scale_lds + q * 256 : dummy_lds + wave_all * 256) - lds_all));
+      x_stride[s] = uniform(live ? kScaleStage : 0);
+    });
+  }
+  auto load_scales = [&](int kt, int st, auto sc) {
+    if constexpr (Lds::kMx) {
+      constexpr int s = decltype(sc)::value;
+      const int q = wave + s * kWaves;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(q < kQA ? rsA : rsB, (lds_void*)(lds_all + x_to[s] + st * x_stride[s]), 4,
+                                               x_voff[s], x_base[s] + kt * x_ld[s], 0, 0);
+    } else {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_q, (lds_void*)(q_to + st * q_stride), 4, q_voff,
+                                               q_base + kt * q_ld, 0, 0);
+    }
   };
+  auto load_all_scales = [&](int kt, int st) { static_for<kMxLoads>([&](auto sc) { load_scales(kt, st, sc); }); };
 
   const TileLoader<BM, kWaves> ldA(g.A, g.lda, m0, g.M, wave);
   int64_t b_row0 = n0;
@@ -721,13 +772,13 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
   auto prologue = [&]() {
     if constexpr (kStages == 2) {
       // stage 0, then stage 1's B tile (see the schedule below)
-      if constexpr (kBlockScaled) load_scales(kb(0), 0);
+      if constexpr (kBlockScaled) load_all_scales(kb(0), 0);
       ldA.load(kb(0) * kBK, lds, wave);
       ldB.load(kb(0) * kBK, lds + kTileA, wave);
       if (KT > 1) ldB.load(kb(1) * kBK, lds + kStage + kTileA, wave);
     } else {
       for (int st = 0; st < kStages - 1 && st < KT; ++st) {
-        if constexpr (kBlockScaled) load_scales(kb(st), st);
+        if constexpr (kBlockScaled) load_all_scales(kb(st), st);
         ldA.load(kb(st) * kBK, lds + st * kStage, wave);
         ldB.load(kb(st) * kBK, lds + st * kStage + kTileA, wave);
       }
@@ -745,7 +796,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
   // wave on the vector-memory queue, which drains at about 64 bytes per clock
   // per CU.
   constexpr int kPerA = TileLoader<BM, kWaves>::kPerWave, kPerB = TileLoader<BN, kWaves>::kPerWave;
-  constexpr int kS0 = kBlockScaled ? 1 : 0;
+  constexpr int kS0 = kBlockScaled ? kMxLoads : 0;
   constexpr int kSlots = kS0 + kPerA + kPerB;
   // kPre slots go out right after the barrier, while the wave waits for its
   // first fragments; the rest kPerStrip per strip
@@ -762,7 +813,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
   constexpr int kNA = kS0 + kPerA;                                   // A-part slots
   constexpr int kPerStripA = (kNA - kPre + TI / 2 - 1) / (TI / 2) > 1 ? (kNA - kPre + TI / 2 - 1) / (TI / 2) : 1;
   constexpr int kPerStripB = (kPerB + TI / 2 - 1) / (TI / 2);        // strips TI/2 .. TI-1
-  static_assert(kQ <= kWaves, "at most one scale-vector load per wave and step");
+  static_assert(kQ <= kWaves || Lds::kMx, "at most one scale-vector load per wave and step");
   // LDS reads of the step's scales, issued after the first strip's MFMAs
   // (1x128 x 1x128: the column scales, two row scales and a fragment at most)
   constexpr int kScaleReads = PAIR == kPairBlock ? TI + (GATED ? 2 : 1) : 0;
@@ -808,7 +859,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
     auto issue_slot = [&](auto sc, auto kb_c) {  // slot S; kb_c: B tile two stages ahead
       constexpr int S = decltype(sc)::value;
       if constexpr (S < kS0)
-        load_scales(kb(kt + kStages - 1), nxt_st);
+        load_scales(kb(kt + kStages - 1), nxt_st, std::integral_constant<int, (S < kMxLoads ? S : 0)>{});
       else if constexpr (S - kS0 < kPerA)
         ldA.template load_group<(S - kS0 < kPerA ? S - kS0 : 0)>(k_nxt, nxt, wave);
       else if constexpr (decltype(kb_c)::value)
@@ -876,12 +927,23 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
       sb_e = lds_read_f32(lds_addr(cur_scales + kScaleA) + (wn / 128) * 4, 0);
       sa_e[0] = lds_read_f32(sa_addr, 0);
     }
+    // E2M1: a lane's row has two scale bytes in each of them, for the two chunks of its
+    // fragments; the second strip's fragment is read after the first product, so that the
+    // reads in flight fit their counter
+    const int mx_at = (lane & 15) * 8 + (lane >> 4) * 2;
+    const uint32_t mx_a = lds_addr(cur_scales) + wm * 8 + mx_at;
+    int sa_m[TI], sb_m[TJ];
+    if constexpr (PAIR == kPairMx4) {
+      const uint32_t mx_b = lds_addr(cur_scales + kScaleA) + wn * 8 + mx_at;
+      static_for<TJ>([&](auto j) { sb_m[j] = lds_read_u16(mx_b, j * 128); });
+      sa_m[0] = lds_read_u16(mx_a, 0);
+    }
     v8i af = read_frag<0>(fa, none, none, done);
     v8i bf[TJ];
     static_for<TJ>([&](auto j) { bf[j] = read_frag<j * 2048>(fb, none, none, done); });
     v8i af_next = af;
-    if constexpr (TI > 1) af_next = read_frag<2048>(fa, none, none, done);
-    constexpr int kNextReads = TI > 1 ? 2 : 0;
+    if constexpr (TI > 1 && PAIR != kPairMx4) af_next = read_frag<2048>(fa, none, none, done);
+    constexpr int kNextReads = TI > 1 && PAIR != kPairMx4 ? 2 : 0;
     issue_strip(std::integral_constant<int, -1>{});
     auto wait_b = [&](auto jc) {  // before strip 0's MFMA with B fragment j
       constexpr int j = decltype(jc)::value;
@@ -905,7 +967,59 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
       if constexpr (GATED) asm volatile("" : "+v"(sb1));
     };
 
-    if constexpr (!kPromote) {
+    if constexpr (PAIR == kPairMx4) {
+      // As below, with two instructions a tile, of one chunk of the fragments each; strip
+      // i + 1's scale bytes are read just before the fragment of strip i + 2.
+      static_for<TI>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        auto product = [&](auto jc, auto hc) {
+          constexpr int j = decltype(jc)::value, h = decltype(hc)::value;
+          acc[i][j] = mfma_16x16x128_mx4<h>(half_frag<h>(bf[j]), half_frag<h>(af), acc[i][j], sb_m[j], sa_m[i]);
+        };
+        const std::integral_constant<int, 0> first{};
+        const std::integral_constant<int, 1> second{};
+        if constexpr (i == 0) {
+          static_for<TJ>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            constexpr int kNext = TI > 1 && j > 0 ? 3 : 0;  // reads of strip 1
+            if constexpr (j == 0) {
+              lds_wait2<2 * (TJ - 1)>(af, bf[0]);
+              static_for<TJ>([&](auto q) { lds_arrived(sb_m[q]); });
+              lds_arrived(sa_m[0]);
+              if constexpr (TI > 1) {
+                sa_m[1] = lds_read_u16(mx_a, 128);
+                af_next = read_frag<2048>(fa, af, bf[0], done);
+              }
+            } else {
+              lds_wait<2 * (TJ - 1 - j) + kNext>(bf[j]);
+            }
+            product(jc, first);
+            product(jc, second);
+            after_mfma(ic, jc);
+          });
+          mid_barrier();
+        } else {
+          static_for<TJ>([&](auto jc) { product(jc, first); });
+          static_for<TJ>([&](auto jc) {
+            product(jc, second);
+            after_mfma(ic, jc);
+          });
+        }
+        v8i af_after = af_next;
+        if constexpr (i + 2 < TI) {
+          if constexpr (i > 0) done = acc[i - 1][TJ - 1][3] * 0.0f;
+          sa_m[i + 2] = lds_read_u16(mx_a, (i + 2) * 128);
+          af_after = read_frag<(i + 2) * 2048>(fa, af, af_next, done);
+          lds_wait<3>(af_next);
+        } else if constexpr (i + 1 < TI) {
+          lds_wait<0>(af_next);
+        }
+        if constexpr (i + 1 < TI) lds_arrived(sa_m[i + 1]);
+        af = af_next;
+        af_next = af_after;
+      });
+      done = acc[TI - 1][TJ - 1][3] * 0.0f;
+    } else if constexpr (!kPromote) {
       // Whole-K accumulation in the MFMA accumulator.  Strip i multiplies
       // with af; the fragment of strip i+2 is read into registers that are
       // neither af nor af_next (early clobber against them via `busy`) once
@@ -1261,6 +1375,7 @@ struct ThinLds {
 // gemm_tile; the first half of the tile's columns are the gate's.
 template <int PAIR, int TI, int TJ, bool QOUT, int FMT, bool GATED = false>
 __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int tm, int tn) {
+  constexpr bool kMx = PAIR == kPairMx4;
   constexpr bool kBlockScaled = PAIR == kPairBlock || PAIR == kPairBlockK || PAIR == kPairBlockE8;
   constexpr bool kWeightBlocks = PAIR == kPairBlock || PAIR == kPairBlockE8;
   static_assert(TJ <= 8 && 8 % TJ == 0, "a tile's columns lie in one 128-column weight block");
@@ -1282,7 +1397,17 @@ __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int t
   // past M (columns past N) fall on other scales or past the array (zero):
   // they only meet partials that are never stored.
   float sa[TI], sb[kColScales];
+  int xa[TI], xb[TJ];  // E2M1: the two scale bytes of this lane's row in each fragment
   auto issue = [&](int kb) {
+    if constexpr (kMx) {
+      const int at = row * 8 + grp * 2;
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+        xa[i] = __builtin_amdgcn_raw_buffer_load_b16(rsA, ((int)m0 + i * 16) * 8 + at + kb * (int)g.sa_ld * 4, 0, 0);
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+        xb[j] = __builtin_amdgcn_raw_buffer_load_b16(rsB, ((int)n0 + j * 16) * 8 + at + kb * (int)g.sb_ld * 4, 0, 0);
+    }
     if constexpr (kBlockScaled) {
 #pragma unroll
       for (int i = 0; i < TI; ++i) sa[i] = load_f32(rsA, ((int)m0 + i * 16 + row + kb * (int)g.sa_ld) * 4, 0);
@@ -1331,6 +1456,13 @@ __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int t
     for (int i = 0; i < TI; ++i) ca[i] = sa[i];
 #pragma unroll
     for (int q = 0; q < kColScales; ++q) cb[q] = sb[q];
+    int ya[TI], yb[TJ];
+    if constexpr (kMx) {
+#pragma unroll
+      for (int i = 0; i < TI; ++i) ya[i] = xa[i];
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) yb[j] = xb[j];
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read: the stage is free
     if (kb + W < kblocks) issue(kb + W);
     const v4f zero = {0.f, 0.f, 0.f, 0.f};
@@ -1338,7 +1470,10 @@ __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int t
     for (int i = 0; i < TI; ++i)
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
-        if constexpr (PAIR == kPairBlockE8) {
+        if constexpr (kMx) {
+          acc[i][j] = mfma_16x16x128_mx4<0>(half_frag<0>(bf[j]), half_frag<0>(af[i]), acc[i][j], yb[j], ya[i]);
+          acc[i][j] = mfma_16x16x128_mx4<1>(half_frag<1>(bf[j]), half_frag<1>(af[i]), acc[i][j], yb[j], ya[i]);
+        } else if constexpr (PAIR == kPairBlockE8) {
           acc[i][j] = mfma_16x16x128_e8(bf[j], af[i], acc[i][j], e8m0_of(cb[0]), e8m0_of(ca[i]));
         } else if constexpr (!kBlockScaled) {
           acc[i][j] = mfma_16x16x128<FMT>(bf[j], af[i], acc[i][j]);

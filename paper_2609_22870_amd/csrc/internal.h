@@ -64,8 +64,11 @@ struct GemmArgs {
 };
 
 // kPairBlockE8: 1x128 x 128x128 with power-of-two scales (applied inside
-// the matrix instruction)
-enum GemmPair { kPairTensor = 0, kPairRow = 1, kPairBlock = 2, kPairBlockK = 3, kPairBlockE8 = 4 };
+// the matrix instruction).  kPairMx4: E2M1 codes with an E8M0 scale per 32 of
+// both operands (fp8q_gemm_mx4): K, lda and ldb are in bytes, two codes each, and sA
+// and sB hold the scale bytes, [K / 128][rows][8] (so sa_ld is 2 rows, in floats).
+// (5 is dispatch.h's kFormQuantized.)
+enum GemmPair { kPairTensor = 0, kPairRow = 1, kPairBlock = 2, kPairBlockK = 3, kPairBlockE8 = 4, kPairMx4 = 6 };
 
 // formats: bit 0 = A's codes are E5M2, bit 1 = B's (kPairBlock and
 // kPairBlockK only; 0 for E4M3 x E4M3).
