@@ -714,13 +714,13 @@ enum { FP8Q_ACCUMULATE = 32u };
 /*
  * The table's gradient from that of y (dy bf16 [T][lddy]): dweight[v] = scale times the
  * sum of dy[t] over the tokens t that are v, [V][ldw] in dtype, summed in fp32 in one order
- * that depends on T and the tokens alone (the results are the same on every run) and rounded
- * once.  Rows of tokens that do not occur are zero; with FP8Q_ACCUMULATE (flags) they are
+ * that depends on the sizes and the tokens alone (the results are the same on every run) and
+ * rounded once.  Rows of tokens that do not occur are zero; with FP8Q_ACCUMULATE (flags) they are
  * not touched, and the others get the sum added in fp32 to what they hold.  Tokens outside
  * 0 .. V-1 take no part (their rows of dy are not read).
  * workspace: at least fp8q_embedding_backward_workspace(T, V, C) bytes, 16-byte aligned,
  * overwritten (calls that share one must be ordered).  Shape rules: C % 16 == 0, T below 2^22,
- * V C below 2^40 (else FP8Q_ERR_UNSUPPORTED).  Alignment: as fp8q_embedding.  dweight must not
+ * V C below 2^33, T ceil(C / 2048) up to 2^25 (else FP8Q_ERR_UNSUPPORTED).  Alignment: as fp8q_embedding.  dweight must not
  * overlap dy.
  */
 fp8q_status fp8q_embedding_backward(const void *dy, int64_t lddy,

@@ -142,9 +142,10 @@ fp8q_status fp8q_embedding(const void* weight, fp8q_dtype dtype, int64_t V, int6
 }
 
 int64_t fp8q_embedding_backward_workspace(int64_t T, int64_t V, int64_t C) {
-  if (T <= 0 || V <= 0 || C <= 0 || T > kMaxRows || !dims_ok(V, C) || C % 16 || V * C >= ((int64_t)1 << 40)) return -1;
-  // workgroups of the sums: chunks of 32 tokens or more and groups of eight rows, by bands of 2048 columns
-  if (((T + 31) / 32 + (V + 7) / 8) * ((C + 2047) / 2048) > kMaxGroups) return -1;
+  if (T <= 0 || V <= 0 || C <= 0 || T > kMaxRows || !dims_ok(V, C) || C % 16 || V * C >= ((int64_t)1 << 33)) return -1;
+  // workgroups of the sums, chunks of eight tokens or more by bands of 2048 columns, beside those
+  // that fill, of 256 pieces of 16 bytes: less than 2^32 threads together
+  if (T * ((C + 2047) / 2048) > ((int64_t)1 << 25)) return -1;
   return fp8q::embedding_backward_workspace(T, V, C);
 }
 
@@ -178,7 +179,7 @@ fp8q_status fp8q_embedding_backward(const void* dy, int64_t lddy, const int64_t*
 
 int64_t fp8q_top_logprobs_workspace(int64_t T, int64_t V, int64_t k) {
   if (T <= 0 || V <= 0 || T > kMaxRows || V > kMaxDim || k < 1 || k > FP8Q_MAX_TOP || k > V) return -1;
-  return fp8q::top_logprobs_workspace(T, V, k);
+  return fp8q::top_logprobs_workspace(T, V);
 }
 
 fp8q_status fp8q_top_logprobs(const void* logits, fp8q_dtype dtype, int64_t T, int64_t V, int64_t ld,

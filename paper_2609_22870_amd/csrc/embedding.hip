@@ -6,12 +6,12 @@
 //
 // The gradient sums each row in the order of t, in fp32, so that every run gives the same
 // bits: the tokens are sorted (stably: by token, then by t), the sorted positions are cut into
-// chunks of kChunk, and a workgroup adds up the rows of dy of one chunk, over a band of columns,
-// run by run of equal tokens.  A run inside a chunk goes to the table at once; one that crosses
-// chunks leaves a sum per chunk in the workspace, and a second kernel adds those in order.
-// The rows of tokens that do not occur are filled with zeros by the same launch (a bitmap of
-// those that do comes with the sort), which is most of what a whole gradient costs: bound by
-// HBM, V C elements written and T C read.
+// chunks, and a workgroup adds up the rows of dy of one chunk, over a band of columns, run by
+// run of equal tokens.  A run inside a chunk goes to the table at once; one that crosses chunks
+// leaves a sum per chunk in the workspace, and a second kernel adds those in order.  The rows of
+// tokens that do not occur are filled with zeros by the launch of the sums (the sort leaves a bitmap of
+// those that do): most of what a whole gradient costs.  Bound by HBM, V C elements written and T C
+// read.
 #include "device_common.h"
 #include "rollout.h"
 
@@ -92,17 +92,20 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(EmbeddingArgs a, in
 // the key V.  A wave ranks 64 keys at a time, in order: the lanes with its digit are found by
 // a ballot per bit, the count of those before them in the wave from a counter in LDS.
 
-// The lanes whose BITS-bit digit is this lane's (of those that are live).
+// The lanes whose BITS-bit digit is this lane's (of those that are live): a bit's ballot,
+// inverted in the lanes that have it clear, leaves the others out.
 template <int BITS>
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool live) {
-  uint64_t m = __ballot(live);
+  const uint64_t all = __ballot(live);
+  uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
 #pragma unroll
   for (int b = 0; b < BITS; ++b) {
-    const bool one = digit >> b & 1;
-    const uint64_t o = __ballot(one);
-    m &= one ? o : ~o;
+    const uint32_t clear = (digit >> b & 1) - 1;  // all ones where the bit is clear
+    const uint64_t o = __ballot(clear == 0);
+    lo &= (uint32_t)o ^ clear;
+    hi &= (uint32_t)(o >> 32) ^ clear;
   }
-  return m;
+  return (uint64_t)hi << 32 | lo;
 }
 
 // A wave's LDS operations before this point come before those after it, for all its lanes.
@@ -112,105 +115,157 @@ __device__ __forceinline__ void in_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// This lane's place among its wave's keys of the same digit so far (counter: the wave's, of
-// this digit), and the counter moved on.
+// This lane's place among its wave's keys of the same digit so far (counters: the wave's, by
+// digit), and the counter moved on.
 template <int BITS>
 __device__ __forceinline__ uint32_t rank_in_wave(uint32_t digit, bool live, uint32_t* counters) {
-  const int lane = threadIdx.x & 63;
   const uint64_t m = same_digit<BITS>(digit, live);
-  const uint64_t below = m & (((uint64_t)1 << lane) - 1);
+  const uint32_t below =
+      __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
   uint32_t before = 0;
   if (live) before = counters[digit];
   in_order();
   if (live && below == 0) counters[digit] = before + (uint32_t)__popcll(m);
   in_order();
-  return before + (uint32_t)__popcll(below);
-}
-
-// Exclusive prefix sums of n counters in LDS by THREADS threads, n a multiple of THREADS.
-template <int THREADS>
-__device__ __forceinline__ void prefix_sums(uint32_t* counters, int n, uint32_t* wave_sums) {
-  const int t = threadIdx.x, lane = t & 63, per = n / THREADS;
-  uint32_t sum = 0;
-  for (int i = 0; i < per; ++i) sum += counters[t * per + i];
-  uint32_t scan = sum;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint32_t o = __shfl_up(scan, d, 64);
-    if (lane >= d) scan += o;
-  }
-  if (lane == 63) wave_sums[t >> 6] = scan;
-  __syncthreads();
-  uint32_t base = scan - sum;
-  for (int w = 0; w < t >> 6; ++w) base += wave_sums[w];
-  for (int i = 0; i < per; ++i) {
-    const uint32_t c = counters[t * per + i];
-    counters[t * per + i] = base;
-    base += c;
-  }
-  __syncthreads();
+  return before + below;
 }
 
 __device__ __forceinline__ uint32_t key_of(int64_t token, int64_t V) {
   return token >= 0 && token < V ? (uint32_t)token : (uint32_t)V;
 }
 
-// Up to kSortMost tokens in one workgroup: a word holds key and t together (kPosBits for
-// t), so the pass that a key makes is one word through LDS.  Wave w has the words from w
-// 64 rounds on, so that its rounds go in order.
+// Which tokens occur: bit v / 8 of part v % 8, parts of used_words(V) words.
+constexpr int kClasses = 8;
+__host__ __device__ constexpr int64_t used_words(int64_t V) { return (V + 32 * kClasses - 1) / (32 * kClasses); }
+
+// Up to kSortMost tokens: workgroup g takes those with token % 8 = g out of all and sorts them by
+// token / 8, its place in the whole being after those of the workgroups before it (equal
+// tokens stay together, which is all that the sums ask for; 16384 tokens with frequencies of 1 / rank in one
+// workgroup 25 us).  Tokens outside the vocabulary are the last of the last class.  A word holds
+// key and t together (kPosBits for t), so the pass that a key makes is one word through LDS.  Wave w has the words
+// from w 64 rounds on, so that its rounds go in order.
 constexpr int kSortThreads = 1024, kSortWaves = 16, kSortRounds = 16, kPosBits = 14;
-constexpr int64_t kSortMost = 16384;
-constexpr int kDigit = 6;  // bits a pass
+constexpr int64_t kSortMost = 16384, kSortMostV = ((int64_t)1 << (32 - kPosBits + 3)) - 16;
+constexpr int kDigit = 9;  // bits a pass, at most
+constexpr int kUsedLds = 1024;  // words of a part of the bitmap in LDS
 
 __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int64_t* tokens, int T, int64_t V, int key_bits,
                                                                   uint32_t* keys, uint32_t* positions,
-                                                                  uint32_t* bitmap) {
+                                                                  uint32_t* used) {
   __shared__ uint32_t words[kSortMost];
-  __shared__ uint32_t counters[kSortWaves << kDigit], sums[kSortWaves];  // [digit][wave]
-  __shared__ uint32_t mine_lds[kSortWaves][1 << kDigit];
+  __shared__ uint32_t counters[kSortWaves][1 << kDigit], sums[kSortWaves], lower[kSortWaves];
+  __shared__ uint32_t marks[kUsedLds];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int rounds = (T + kSortThreads - 1) / kSortThreads, first = wave * rounds * 64 + lane;
-  for (int64_t i = t; i < (V + 31) / 32; i += kSortThreads) bitmap[i] = 0;
+  const uint32_t g = blockIdx.x;
   uint32_t w[kSortRounds], rank[kSortRounds];
+  int rounds = (T + kSortThreads - 1) / kSortThreads, first = wave * rounds * 64 + lane;
+  const uint32_t outside = (uint32_t)((V + 7) / 8 * 8 + 7);
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
     const int i = first + r * 64;
+    int64_t token = 0;
+    if (r < rounds && i < T) token = tokens[i];
+    rank[r] = token >= 0 && token < V ? (uint32_t)token : outside;
+  }
+  for (int64_t i = t; i < kUsedLds; i += kSortThreads) marks[i] = 0;
+  // this class's words, in order
+  uint32_t own = 0, less = 0;
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r) {
+    const bool live = r < rounds && first + r * 64 < T;
+    own += (uint32_t)__popcll(__ballot(live && (rank[r] & 7) == g));
+    less += (uint32_t)__popcll(__ballot(live && (rank[r] & 7) < g));
+  }
+  if (lane == 0) {
+    sums[wave] = own;
+    lower[wave] = less;
+  }
+  __syncthreads();
+  uint32_t at = 0, place = 0, count = 0;
+#pragma unroll
+  for (int o = 0; o < kSortWaves; ++o) {
+    at += o < wave ? sums[o] : 0;
+    count += sums[o];
+    place += lower[o];
+  }
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r) {
+    const bool mine = r < rounds && first + r * 64 < T && (rank[r] & 7) == g;
+    const uint64_t m = __ballot(mine);
+    if (mine)
+      words[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] =
+          rank[r] >> 3 << kPosBits | (uint32_t)(first + r * 64);
+    at += (uint32_t)__popcll(m);
+  }
+  __syncthreads();
+  const int n = (int)count;
+  rounds = (n + kSortThreads - 1) / kSortThreads;
+  first = wave * rounds * 64 + lane;
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r) {
     w[r] = 0xffffffffu;
-    if (r < rounds && i < T) w[r] = key_of(tokens[i], V) << kPosBits | (uint32_t)i;
+    if (r < rounds && first + r * 64 < n) w[r] = words[first + r * 64];
   }
-  uint32_t* const mine = mine_lds[wave];
-  for (int shift = 0; shift < key_bits; shift += kDigit) {
-    mine[lane] = 0;
+  const int passes = (key_bits + kDigit - 1) / kDigit, bits = (key_bits + passes - 1) / passes;
+  uint32_t* const mine = counters[wave];
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = kPosBits + pass * bits;
+    auto digit_of = [&](uint32_t x) { return x >> shift & ((1u << bits) - 1); };
+    for (int d = lane; d < 1 << kDigit; d += 64) mine[d] = 0;
     in_order();
-    auto digit_of = [&](uint32_t x) { return x >> (kPosBits + shift) & ((1u << kDigit) - 1); };
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r)
-      if (r < rounds) rank[r] = rank_in_wave<kDigit>(digit_of(w[r]), first + r * 64 < T, mine);
+      if (r < rounds) rank[r] = rank_in_wave<kDigit>(digit_of(w[r]), first + r * 64 < n, mine);
     __syncthreads();
-    counters[lane * kSortWaves + wave] = mine[lane];
+    // prefix sums over the digits, and over the waves of a digit: two threads a digit
+    constexpr int kPer = kSortWaves / 2;
+    static_assert(2 << kDigit == kSortThreads);
+    uint32_t c[kPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      c[i] = counters[(t & 1) * kPer + i][t >> 1];
+      sum += c[i];
+    }
+    uint32_t scan = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint32_t o = __shfl_up(scan, d, 64);
+      if (lane >= d) scan += o;
+    }
+    if (lane == 63) sums[wave] = scan;
     __syncthreads();
-    prefix_sums<kSortThreads>(counters, kSortWaves << kDigit, sums);
+    uint32_t base = scan - sum;
+#pragma unroll
+    for (int o = 0; o < kSortWaves; ++o) base += o < wave ? sums[o] : 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      counters[(t & 1) * kPer + i][t >> 1] = base;
+      base += c[i];
+    }
+    __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r)
-      if (r < rounds && first + r * 64 < T) words[counters[digit_of(w[r]) * kSortWaves + wave] + rank[r]] = w[r];
+      if (r < rounds && first + r * 64 < n) words[mine[digit_of(w[r])] + rank[r]] = w[r];
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r)
-      if (r < rounds && first + r * 64 < T) w[r] = words[first + r * 64];
-    __syncthreads();
+      if (r < rounds && first + r * 64 < n) w[r] = words[first + r * 64];
+    // (the next pass writes the words again only after more barriers)
   }
-  // (the bitmap's zeros are in memory: a barrier waits for the workgroup's own stores)
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
     const int i = first + r * 64;
-    if (r < rounds && i < T) {
-      const uint32_t key = w[r] >> kPosBits;
-      keys[i] = key;
-      positions[i] = w[r] & ((1u << kPosBits) - 1);
-      if (key < (uint32_t)V && (i == 0 || words[i - 1] >> kPosBits != key))
-        __hip_atomic_fetch_or(bitmap + (key >> 5), 1u << (key & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (r < rounds && i < n) {
+      const uint32_t high = w[r] >> kPosBits, key = high << 3 | g;
+      keys[place + i] = key;
+      positions[place + i] = w[r] & ((1u << kPosBits) - 1);
+      if (key < (uint32_t)V)
+        __hip_atomic_fetch_or(marks + (high >> 5), 1u << (high & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
   }
+  __syncthreads();
+  const int64_t part = used_words(V);
+  for (int64_t i = t; i < part; i += kSortThreads) used[g * part + i] = marks[i];
 }
 
 // More tokens: tiles of kTile in a workgroup each, a pass being three launches (the tiles'
@@ -225,7 +280,7 @@ struct SortPass {
   uint32_t* counts;  // [256][tiles]
   int64_t T, V;
   int tiles, shift;
-  uint32_t* bitmap;  // of the last pass, else null
+  uint32_t* used;  // of the last pass, else null
   __device__ __forceinline__ uint32_t key(int64_t i) const { return tokens ? key_of(tokens[i], V) : keys[i]; }
   __device__ __forceinline__ uint32_t digit(uint32_t k) const { return k >> shift & ((1u << kWideDigit) - 1); }
 };
@@ -243,10 +298,10 @@ __global__ __launch_bounds__(kTileThreads) void sort_count_kernel(SortPass p) {
   }
   __syncthreads();
   p.counts[(int64_t)t * p.tiles + blockIdx.x] = counts[t];
-  if (p.bitmap)
-    for (int64_t i = first; i < (p.V + 31) / 32; i += (int64_t)gridDim.x * kTile)
-      for (int r = 0; r < kTileRounds; ++r)
-        if (i + r * kTileThreads < (p.V + 31) / 32) p.bitmap[i + r * kTileThreads] = 0;
+  if (p.used)
+    for (int64_t i = (int64_t)blockIdx.x * kTileThreads + t; i < kClasses * used_words(p.V);
+         i += (int64_t)gridDim.x * kTileThreads)
+      p.used[i] = 0;
 }
 
 // Exclusive prefix sums of n counts, by one workgroup.
@@ -319,119 +374,172 @@ __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(SortPass p) {
     const uint32_t to = counters[wave][p.digit(key[r])] + rank[r];
     p.keys_out[to] = key[r];
     p.positions_out[to] = p.tokens ? (uint32_t)i : p.positions[i];
-    if (p.bitmap && key[r] < (uint32_t)p.V)
-      __hip_atomic_fetch_or(p.bitmap + (key[r] >> 5), 1u << (key[r] & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (p.used && key[r] < (uint32_t)p.V) {
+      const uint32_t high = key[r] >> 3;
+      __hip_atomic_fetch_or(p.used + (key[r] & 7) * used_words(p.V) + (high >> 5), 1u << (high & 31), __ATOMIC_RELAXED,
+                            __HIP_MEMORY_SCOPE_AGENT);
+    }
   }
 }
 
 // ---- the sums -----------------------------------------------------------------------------
 
+// n / d for n below 2^36, d below 2^29, by a product: with k = 36 + the bits of d, m = ceil(2^k /
+// d) is off by less than d, so n m / 2^k by less than 1 / d.
+struct Divisor {
+  uint32_t d;
+  int shift;
+  uint64_t m;
+  explicit Divisor(uint32_t d_ = 1) : d(d_), shift(36) {
+    while ((uint64_t)1 << (shift - 36) < d) ++shift;
+    m = (uint64_t)((((unsigned __int128)1 << shift) + d - 1) / d);
+  }
+  __device__ __forceinline__ uint64_t quotient(uint64_t n) const {
+    const uint64_t lo = n * m, hi = __umul64hi(n, m);
+    return shift >= 64 ? hi >> (shift - 64) : hi << (64 - shift) | lo >> shift;
+  }
+};
+
 struct Gradient {
   EmbeddingBackwardArgs a;
-  const uint32_t *keys, *positions, *bitmap;
+  const uint32_t *keys, *positions, *used;
   float* partials;  // [chunks][2][C]: the sums of a run from the chunk before, and of one into the next
   int chunk;        // positions of a chunk
   int chunks, bands;
+  Divisor row;      // 16-byte pieces of a row of the table
 };
 
-// Columns c .. c + 7 of row v of the table.
-__device__ __forceinline__ void put_row(const EmbeddingBackwardArgs& a, uint32_t v, int64_t c, const Eight& sum) {
+// Zeros in the rows that no token names: one 16-byte piece a thread, workgroup after workgroup
+// along the table (2 GiB at 6.7 TB/s; four pieces a thread 6.0, rows of a range a workgroup 5.8,
+// workgroups that stay 4.9 to 5.8).
+template <bool F32>
+__global__ __launch_bounds__(kThreads) void embedding_fill_kernel(Gradient g) {
+  const EmbeddingBackwardArgs& a = g.a;
+  const unsigned group = blockIdx.x;
+  constexpr int kN = F32 ? 4 : 8;
+  // the workgroup's first piece's row, and this thread's from there
+  const uint64_t first = (uint64_t)group * kThreads;
+  uint64_t v = g.row.quotient(first);
+  int64_t c = (int64_t)(first - v * g.row.d) + threadIdx.x;
+  const uint32_t more = g.row.quotient((uint64_t)c);
+  v += more;
+  c -= (int64_t)more * g.row.d;
+  if (v >= (uint64_t)a.V) return;
+  if (g.used[(v & 7) * used_words(a.V) + (v >> 8)] >> (v >> 3 & 31) & 1) return;
+  const int64_t at = (int64_t)v * a.ldw + c * kN;
+  const v4u zero = {0, 0, 0, 0};
+  if constexpr (F32)
+    *reinterpret_cast<v4u*>(static_cast<float*>(a.dweight) + at) = zero;
+  else
+    *reinterpret_cast<v4u*>(static_cast<uint16_t*>(a.dweight) + at) = zero;
+}
+
+// A thread's eight columns of a band, in two pieces of four: side by side for a bf16 table,
+// kHalf apart for an fp32 one, so that a store of four is beside its neighbours'.
+constexpr int kHalf = kBand / 2;
+template <bool F32>
+__device__ __forceinline__ int64_t column(int64_t band) {
+  return band * kBand + threadIdx.x * (F32 ? 4 : 8);
+}
+
+template <bool F32>
+__device__ __forceinline__ Eight load_dy(const uint16_t* row, bool second) {
+  Eight x;
+  if constexpr (F32) {
+    const uint2 lo = *reinterpret_cast<const uint2*>(row);
+    const uint2 hi = second ? *reinterpret_cast<const uint2*>(row + kHalf) : make_uint2(0, 0);
+    x.widen(v4u{lo.x, lo.y, hi.x, hi.y});
+  } else {
+    x.widen(*reinterpret_cast<const v4u*>(row));
+  }
+  return x;
+}
+
+// What the columns of row v of the table from c on hold (second: the other four are inside it, too).
+template <bool F32>
+__device__ __forceinline__ Eight load_row(const EmbeddingBackwardArgs& a, uint32_t v, int64_t c, bool second) {
+  const int64_t at = (int64_t)v * a.ldw + c;
+  Eight x{};
+  if constexpr (F32) {
+    const float* const from = static_cast<const float*>(a.dweight) + at;
+    const v4u lo = *reinterpret_cast<const v4u*>(from);
+    const v4u hi = second ? *reinterpret_cast<const v4u*>(from + kHalf) : v4u{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x.v[e] = __uint_as_float(lo[e]);
+      x.v[4 + e] = __uint_as_float(hi[e]);
+    }
+  } else {
+    x.widen(*reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(a.dweight) + at));
+  }
+  return x;
+}
+
+template <bool F32, bool ADD>
+__device__ __forceinline__ void put_row(const EmbeddingBackwardArgs& a, uint32_t v, int64_t c, bool second,
+                                        const Eight& sum, const Eight& old) {
+  const int64_t at = (int64_t)v * a.ldw + c;
   Eight x;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x.v[e] = sum.v[e] * a.scale;
-  const int64_t at = (int64_t)v * a.ldw + c;
-  if (a.f32) {
-    v4u* const to = reinterpret_cast<v4u*>(static_cast<float*>(a.dweight) + at);
+  for (int e = 0; e < 8; ++e) x.v[e] = ADD ? old.v[e] + sum.v[e] * a.scale : sum.v[e] * a.scale;
+  if constexpr (F32) {
+    float* const to = static_cast<float*>(a.dweight) + at;
     v4u lo, hi;
-    if (a.accumulate) {
-      lo = to[0];
-      hi = to[1];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x.v[e] += __uint_as_float(lo[e]);
-        x.v[4 + e] += __uint_as_float(hi[e]);
-      }
-    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       lo[e] = __float_as_uint(x.v[e]);
       hi[e] = __float_as_uint(x.v[4 + e]);
     }
-    __builtin_nontemporal_store(lo, to);
-    __builtin_nontemporal_store(hi, to + 1);
+    __builtin_nontemporal_store(lo, reinterpret_cast<v4u*>(to));
+    if (second) __builtin_nontemporal_store(hi, reinterpret_cast<v4u*>(to + kHalf));
   } else {
-    v4u* const to = reinterpret_cast<v4u*>(static_cast<uint16_t*>(a.dweight) + at);
-    if (a.accumulate) {
-      Eight old;
-      old.widen(*to);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x.v[e] += old.v[e];
-    }
-    __builtin_nontemporal_store(x.narrow(), to);
+    __builtin_nontemporal_store(x.narrow(), reinterpret_cast<v4u*>(static_cast<uint16_t*>(a.dweight) + at));
   }
 }
 
-// The first chunks * bands workgroups sum a chunk over a band of columns each; the others fill
-// kFillRows rows of the table with zeros where no token names them.
-constexpr int kFillRows = 8, kAhead = 8;  // rows of dy in flight
+// A workgroup sums a chunk over a band of columns, kAhead positions at a time: their rows of dy
+// and, to be added to, the table's rows of the runs that end there are all in flight together.
+constexpr int kChunk = 8;  // a chunk has a multiple of it
 
+template <bool F32, bool ADD>
 __global__ __launch_bounds__(kThreads) void embedding_sums_kernel(Gradient g) {
   const EmbeddingBackwardArgs& a = g.a;
-  const unsigned sums = (unsigned)g.chunks * g.bands;
-  const unsigned b = blockIdx.x < sums ? blockIdx.x : blockIdx.x - sums;
-  const int64_t c = (int64_t)(b % g.bands) * kBand + threadIdx.x * 8;
+  const int64_t j = blockIdx.x / g.bands, c = column<F32>(blockIdx.x % g.bands);
   if (c >= a.C) return;
-  if (blockIdx.x >= sums) {
-    const int64_t v0 = (int64_t)(b / g.bands) * kFillRows;  // (a word of the bitmap has whole groups)
-    const uint32_t used = g.bitmap[v0 >> 5] >> (v0 & 31);
-    const v4u zero = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < kFillRows; ++i) {
-      if (v0 + i >= a.V || (used >> i & 1)) continue;
-      const int64_t at = (v0 + i) * a.ldw + c;
-      if (a.f32) {
-        v4u* const to = reinterpret_cast<v4u*>(static_cast<float*>(a.dweight) + at);
-        __builtin_nontemporal_store(zero, to);
-        __builtin_nontemporal_store(zero, to + 1);
-      } else {
-        __builtin_nontemporal_store(zero, reinterpret_cast<v4u*>(static_cast<uint16_t*>(a.dweight) + at));
-      }
-    }
-    return;
-  }
-  const int64_t first = (int64_t)(b / g.bands) * g.chunk, last = first + g.chunk < a.T ? first + g.chunk : a.T;
-  float* const part = g.partials + (int64_t)(b / g.bands) * 2 * a.C + c;
+  const bool second = !F32 || c + kHalf < a.C;
+  const int64_t first = j * g.chunk, last = first + g.chunk < a.T ? first + g.chunk : a.T;
+  float* const part = g.partials + j * 2 * a.C + c;
+  const uint32_t V = (uint32_t)a.V;
   bool from_before = first > 0 && g.keys[first - 1] == g.keys[first];
+  constexpr int kAhead = ADD ? 4 : 8;  // (eight with the rows that are added to: 152 registers, 160 us for 122)
   Eight sum{};
   for (int64_t i0 = first; i0 < last; i0 += kAhead) {
-    v4u p[kAhead];
+    Eight x[kAhead], old[kAhead];
     uint32_t key[kAhead + 1];
 #pragma unroll
+    for (int u = 0; u <= kAhead; ++u) key[u] = i0 + u < a.T ? g.keys[i0 + u] : 0xffffffffu;
+#pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int64_t i = i0 + u < last ? i0 + u : last - 1;
-      key[u] = g.keys[i];
-      p[u] = v4u{0, 0, 0, 0};
-      if (key[u] < (uint32_t)a.V)
-        p[u] = __builtin_nontemporal_load(
-            reinterpret_cast<const v4u*>(a.dy + (int64_t)g.positions[i] * a.lddy + c));
+      x[u] = old[u] = Eight{};
+      if (key[u] < V) {
+        x[u] = load_dy<F32>(a.dy + (int64_t)g.positions[i0 + u] * a.lddy + c, second);
+        if (ADD && key[u + 1] != key[u]) old[u] = load_row<F32>(a, key[u], c, second);
+      }
     }
-    key[kAhead] = i0 + kAhead < a.T ? g.keys[i0 + kAhead] : 0xffffffffu;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      if (i0 + u >= last || key[u] >= (uint32_t)a.V) break;  // (the tokens outside come last)
-      Eight x;
-      x.widen(p[u]);
+      if (key[u] >= V) break;  // (the tokens outside come last)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum.v[e] += x.v[e];
-      const bool at_end = i0 + u + 1 == last;
-      const uint32_t next = at_end ? (last < a.T ? g.keys[last] : 0xffffffffu) : key[u + 1];
-      if (next == key[u] && !at_end) continue;
-      if (next != key[u] && !from_before) {
-        put_row(a, key[u], c, sum);
+      for (int e = 0; e < 8; ++e) sum.v[e] += x[u].v[e];
+      const bool ends = key[u + 1] != key[u];
+      if (!ends && i0 + u + 1 != last) continue;
+      if (ends && !from_before) {
+        put_row<F32, ADD>(a, key[u], c, second, sum, old[u]);
       } else {
         float* const to = part + (from_before ? 0 : a.C);
         *reinterpret_cast<float4*>(to) = make_float4(sum.v[0], sum.v[1], sum.v[2], sum.v[3]);
-        *reinterpret_cast<float4*>(to + 4) = make_float4(sum.v[4], sum.v[5], sum.v[6], sum.v[7]);
+        if (second)
+          *reinterpret_cast<float4*>(to + (F32 ? kHalf : 4)) = make_float4(sum.v[4], sum.v[5], sum.v[6], sum.v[7]);
       }
       sum = Eight{};
       from_before = false;
@@ -441,13 +549,13 @@ __global__ __launch_bounds__(kThreads) void embedding_sums_kernel(Gradient g) {
 
 // Workgroup (chunk, band): if a run starts in the chunk and goes on into the next, its sums
 // of all its chunks, added in order.
+template <bool F32, bool ADD>
 __global__ __launch_bounds__(kThreads) void embedding_join_kernel(Gradient g) {
   const EmbeddingBackwardArgs& a = g.a;
-  const int64_t j = blockIdx.x / g.bands, c = (int64_t)(blockIdx.x % g.bands) * kBand + threadIdx.x * 8;
+  const int64_t j = blockIdx.x / g.bands, c = column<F32>(blockIdx.x % g.bands);
   const int64_t next = (j + 1) * g.chunk;  // (below T: the last chunk has no next)
-  const uint32_t key = g.keys[next - 1];
-  if (key >= (uint32_t)a.V || g.keys[next] != key) return;
-  if (j > 0 && g.keys[j * g.chunk - 1] == key) return;  // it started before
+  const uint32_t key = g.keys[next - 1], after = g.keys[next], before = j > 0 ? g.keys[j * g.chunk - 1] : 0xffffffffu;
+  if (key >= (uint32_t)a.V || after != key || before == key) return;  // none, or it started before
   // the chunks after j whose first position is the run's: those up to j + more
   int more = 0;
   for (int64_t base = next;; base += (int64_t)kThreads * g.chunk) {
@@ -457,29 +565,33 @@ __global__ __launch_bounds__(kThreads) void embedding_join_kernel(Gradient g) {
     if (n < kThreads) break;
   }
   if (c >= a.C) return;
+  const bool second = !F32 || c + kHalf < a.C;
   const float* part = g.partials + j * 2 * a.C + c;
   auto load = [&](const float* from) {
-    const float4 lo = *reinterpret_cast<const float4*>(from), hi = *reinterpret_cast<const float4*>(from + 4);
+    const float4 lo = *reinterpret_cast<const float4*>(from);
+    const float4 hi = second ? *reinterpret_cast<const float4*>(from + (F32 ? kHalf : 4)) : make_float4(0, 0, 0, 0);
     return Eight{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}};
   };
-  Eight sum = load(part + a.C);
-  for (int i0 = 1; i0 <= more; i0 += 4) {
-    Eight x[4];
+  Eight sum = load(part + a.C), old{};
+  if (ADD) old = load_row<F32>(a, key, c, second);
+  constexpr int kAhead = 8;
+  for (int i0 = 1; i0 <= more; i0 += kAhead) {
+    Eight x[kAhead];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = load(part + (int64_t)(i0 + u <= more ? i0 + u : more) * 2 * a.C);
+    for (int u = 0; u < kAhead; ++u) x[u] = load(part + (int64_t)(i0 + u <= more ? i0 + u : more) * 2 * a.C);
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < kAhead; ++u)
       if (i0 + u <= more)
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum.v[e] += x[u].v[e];
   }
-  put_row(a, key, c, sum);
+  put_row<F32, ADD>(a, key, c, second, sum, old);
 }
 
-// Positions of a chunk: 32, more where that leaves 2048 chunks or more.
-inline int chunk_of(int64_t T) {
-  int64_t n = 32;
-  while (n * 2048 <= T) n *= 2;
+// Positions of a chunk, a multiple of kChunk: more where that leaves 2048 workgroups or more.
+inline int chunk_of(int64_t T, int64_t C) {
+  int64_t n = kChunk;
+  while (n * 2048 <= T * ((C + kBand - 1) / kBand) && n < ((int64_t)1 << 20)) n *= 2;
   return (int)n;
 }
 
@@ -487,11 +599,11 @@ inline int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
 
 // The workspace's parts, in bytes from its start.
 struct Layout {
-  int64_t keys[2], positions[2], counts, bitmap, partials, bytes;
+  int64_t keys[2], positions[2], counts, used, partials, bytes;
   int tiles;
   bool small;
   Layout(int64_t T, int64_t V, int64_t C) {
-    small = T <= kSortMost && V < ((int64_t)1 << (32 - kPosBits));
+    small = T <= kSortMost && V <= kSortMostV && used_words(V) <= kUsedLds;
     tiles = small ? 0 : (int)((T + kTile - 1) / kTile);
     int64_t at = 0;
     auto take = [&](int64_t n) {
@@ -505,8 +617,8 @@ struct Layout {
       positions[i] = take(used ? 4 * T : 0);
     }
     counts = take((int64_t)4 * tiles << kWideDigit);
-    bitmap = take((V + 31) / 32 * 4);
-    const int64_t n = chunk_of(T);
+    used = take(4 * kClasses * used_words(V));
+    const int64_t n = chunk_of(T, C);
     partials = take((T + n - 1) / n * 2 * C * 4);
     bytes = at;
   }
@@ -537,12 +649,11 @@ int64_t embedding_backward_workspace(int64_t T, int64_t V, int64_t C) { return L
 hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t s) {
   const Layout l(a.T, a.V, a.C);
   auto words = [&](int64_t at) { return reinterpret_cast<uint32_t*>(a.workspace + at); };
-  uint32_t* const bitmap = words(l.bitmap);
   int out = 0;
   hipError_t e;
   if (l.small) {
-    sort_small_kernel<<<1, kSortThreads, 0, s>>>(a.tokens, (int)a.T, a.V, bits_of(a.V), words(l.keys[0]),
-                                                  words(l.positions[0]), bitmap);
+    sort_small_kernel<<<kClasses, kSortThreads, 0, s>>>(a.tokens, (int)a.T, a.V, bits_of((a.V + 7) / 8),
+                                                        words(l.keys[0]), words(l.positions[0]), words(l.used));
     if ((e = hipGetLastError()) != hipSuccess) return e;
   } else {
     const int bits = bits_of(a.V);
@@ -559,7 +670,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t
       p.V = a.V;
       p.tiles = l.tiles;
       p.shift = shift;
-      p.bitmap = shift + kWideDigit >= bits ? bitmap : nullptr;
+      p.used = shift + kWideDigit >= bits ? words(l.used) : nullptr;
       sort_count_kernel<<<l.tiles, kTileThreads, 0, s>>>(p);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       sort_scan_kernel<<<1, kSortThreads, 0, s>>>(p.counts, (int64_t)l.tiles << kWideDigit);
@@ -572,19 +683,31 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t
   g.a = a;
   g.keys = words(l.keys[out]);
   g.positions = words(l.positions[out]);
-  g.bitmap = bitmap;
+  g.used = words(l.used);
   g.partials = reinterpret_cast<float*>(a.workspace + l.partials);
-  g.chunk = chunk_of(a.T);
+  g.chunk = chunk_of(a.T, a.C);
   g.chunks = (int)((a.T + g.chunk - 1) / g.chunk);
   g.bands = (int)((a.C + kBand - 1) / kBand);
-  const int64_t fill = a.accumulate ? 0 : (a.V + kFillRows - 1) / kFillRows;
-  embedding_sums_kernel<<<(unsigned)((g.chunks + fill) * g.bands), kThreads, 0, s>>>(g);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (g.chunks > 1) {
-    embedding_join_kernel<<<(unsigned)((int64_t)(g.chunks - 1) * g.bands), kThreads, 0, s>>>(g);
-    e = hipGetLastError();
-  }
-  return e;
+  g.row = Divisor((uint32_t)(a.C / (a.f32 ? 4 : 8)));
+  const int64_t fill = a.accumulate ? 0 : (a.V * g.row.d + kThreads - 1) / kThreads;
+  const auto launch = [&](auto sums, auto join) {
+    if (fill) {
+      if (a.f32)
+        embedding_fill_kernel<true><<<(unsigned)fill, kThreads, 0, s>>>(g);
+      else
+        embedding_fill_kernel<false><<<(unsigned)fill, kThreads, 0, s>>>(g);
+    }
+    sums<<<(unsigned)(g.chunks * g.bands), kThreads, 0, s>>>(g);
+    const hipError_t st = hipGetLastError();
+    if (st != hipSuccess || g.chunks == 1) return st;
+    join<<<(unsigned)((g.chunks - 1) * g.bands), kThreads, 0, s>>>(g);
+    return hipGetLastError();
+  };
+  if (a.accumulate)
+    return a.f32 ? launch(embedding_sums_kernel<true, true>, embedding_join_kernel<true, true>)
+                 : launch(embedding_sums_kernel<false, true>, embedding_join_kernel<false, true>);
+  return a.f32 ? launch(embedding_sums_kernel<true, false>, embedding_join_kernel<true, false>)
+               : launch(embedding_sums_kernel<false, false>, embedding_join_kernel<false, false>);
 }
 
 }  // namespace fp8q

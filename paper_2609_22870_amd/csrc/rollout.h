@@ -60,15 +60,13 @@ struct EmbeddingBackwardArgs {
 int64_t embedding_backward_workspace(int64_t T, int64_t V, int64_t C);
 hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t s);
 
-constexpr int kTopMost = 64;  // alternatives of a row, at most
-
 struct TopArgs : LossArgs {
   int k;
   int64_t* ids;  // [T][k]
   float* top;    // [T][k]
   uint8_t* workspace;
 };
-int64_t top_logprobs_workspace(int64_t T, int64_t V, int64_t k);
+int64_t top_logprobs_workspace(int64_t T, int64_t V);
 hipError_t launch_top_logprobs(const TopArgs& a, hipStream_t s);
 
 }  // namespace fp8q

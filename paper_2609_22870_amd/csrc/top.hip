@@ -6,13 +6,13 @@
 // by index.  A logit of -inf is no alternative; where a row has fewer than k others, the
 // places left over get the index -1 and -inf.
 //
-// Bound by HBM: the logits read once.  The pass that takes a thread's running maximum and
-// sums leaves each thread's largest logit.  The 64 groups of threads with equal t % 64 have a largest
-// logit each, and the k-th largest of those is at most the row's k-th largest logit (k of them
-// are as large): a bound that a few elements pass, which only threads with a
-// maximum at the bound hold.  Their pieces are read again (from the caches), and what passes
-// is ranked by counting.  Where more pass than LDS has room for (logits that are all equal,
-// say), the k largest are taken one after the other from the row: slower, and right for any row.
+// Bound by HBM: the logits read once.  The pass that takes the running maximum and sums leaves
+// the largest logit of every slot (a thread's elements, or those of 64 in a row that is shared by
+// workgroups).  The slots fall into 64 or 256 groups; the k-th largest of the groups' maxima, cut to 16
+// bits, is at most the row's k-th largest logit (k elements are as large): a bound that few elements pass, all of them
+// in slots whose maximum passes.  Those slots are read again (from the caches), and what passes is
+// ranked by counting.  Where more pass than LDS has room for (logits that are all equal, say),
+// the k largest are taken one after the other from the row: slower, and right for any row.
 #include "logits.h"
 #include "rollout.h"
 
@@ -84,50 +84,71 @@ __device__ __forceinline__ Key wave_max_key(Key k) {
 
 constexpr int kCandidates = 1024;
 
-// LDS of the selection.
-template <int THREADS>
+// LDS of the selection among SLOTS slots.
+template <int THREADS, int SLOTS>
 struct Selection {
   float maxima[THREADS];
-  uint16_t threads[THREADS];
+  uint16_t slots[SLOTS];
   Key keys[kCandidates];
   Key wave_keys[THREADS / 64];
   int selected, candidates;
 };
 
-// The k-th largest of the 64 values that a wave's lanes hold (k <= 64): of equal ones as many
-// as there are.
-__device__ __forceinline__ float kth_of_wave(float v, int k) {
-  int larger = 0, equal = 0;
+// At most the k-th largest of the N values that each of a wave's 64 lanes holds (k <= 64): its
+// upper 16 bits in the logits' order, bit by bit from the top, each by counting the values that reach it.
+template <int N>
+__device__ __forceinline__ float bound_of_wave(const float (&v)[N], int k) {
+  uint32_t o[N], b = 0;
 #pragma unroll
-  for (int l = 0; l < 64; ++l) {
-    const float o = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l));
-    larger += o > v ? 1 : 0;
-    equal += o == v ? 1 : 0;
+  for (int i = 0; i < N; ++i) o[i] = ordered(v[i]) >> 16;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t c = b | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += (int)__popcll(__ballot(o[i] >= c));
+    if (n >= k) b = c;
   }
-  const uint64_t at = __ballot(larger < k && k <= larger + equal);
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), __builtin_ctzll(at)));
+  // (0x7f: those of -inf and NaN)
+  return b <= 0x7f ? kNegInf : logit_of((Key)(b << 16) << 32);
 }
 
-// The k largest elements of a slice of a row (pieces first .. last - 1, and `edge` of every
-// thread, or -1), into the first k of s.keys, in order (0: none).  `most`: the largest that this
-// thread has met in pieces first + t + i THREADS and its edge.
-template <bool F32, int THREADS>
-__device__ __forceinline__ void select_top(Selection<THREADS>& s, const Row<F32>& x, int first, int last, int edge,
-                                           float most, int k) {
-  using P = Piece<F32>;
-  constexpr int W = THREADS / 64;
+// The bound of a row whose slots' maxima are `most` of each thread, in groups by t % 64, or by t
+// % 256 for a large k, where 64 groups let through a multiple of k (about 64 log(64 / (64 - k))
+// elements: 64 x 131072 bf16, k = 64, 54 us, with 256 groups 22; k = 5 15.5 and 16.2).
+template <int THREADS, int SLOTS>
+__device__ __forceinline__ float bound_of(Selection<THREADS, SLOTS>& s, float most, int k) {
   const int t = threadIdx.x, lane = t & 63;
   s.maxima[t] = most;
   if (t == 0) s.selected = s.candidates = 0;
   __syncthreads();
-  float group = s.maxima[lane];
+  float group[4];
 #pragma unroll
-  for (int w = 1; w < W; ++w) group = fmaxf(group, s.maxima[w * 64 + lane]);
-  const float bound = kth_of_wave(group, k);
-  if (most >= bound && most > kNegInf) {
-    const int n = __hip_atomic_fetch_add(&s.selected, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    s.threads[n] = (uint16_t)t;
+  for (int i = 0; i < 4; ++i) {
+    group[i] = s.maxima[i * 64 + lane];
+#pragma unroll
+    for (int w = 4 + i; w < THREADS / 64; w += 4) group[i] = fmaxf(group[i], s.maxima[w * 64 + lane]);
   }
+  if (k > 24) return bound_of_wave(group, k);
+  const float all[1] = {fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]))};
+  return bound_of_wave(all, k);
+}
+
+template <int THREADS, int SLOTS>
+__device__ __forceinline__ void select_slot(Selection<THREADS, SLOTS>& s, int slot, float most, float bound) {
+  if (most >= bound && most > kNegInf)
+    s.slots[__hip_atomic_fetch_add(&s.selected, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)] = (uint16_t)slot;
+}
+
+// The k largest elements of a row, into the first k of s.keys, in order (0: none), after
+// select_slot for every slot.  piece(slot, i): piece i, of `per`, of a slot, or -1; `edge`: this
+// thread's single element, or -1.
+template <bool F32, int THREADS, int SLOTS, typename Slot>
+__device__ __forceinline__ void select_top(Selection<THREADS, SLOTS>& s, const Row<F32>& x, int edge, float bound, int k,
+                                           int per, Slot&& piece) {
+  using P = Piece<F32>;
+  constexpr int W = THREADS / 64;
+  const int t = threadIdx.x, lane = t & 63;
   __syncthreads();
   auto offer = [&](float v, int index) {
     if (v >= bound && v > kNegInf) {
@@ -135,17 +156,18 @@ __device__ __forceinline__ void select_top(Selection<THREADS>& s, const Row<F32>
       if (n < kCandidates) s.keys[n] = key_of(v, (uint32_t)index);
     }
   };
-  // the selected threads' pieces, one a thread at a time (the order does not matter: the
-  // keys are all different)
-  const int per = last > first ? (last - first + THREADS - 1) / THREADS : 0, work = s.selected * per;
-  for (int q = t; q < work; q += THREADS) {
-    const int from = q / per, j = first + s.threads[from] + (q - from * per) * THREADS;
-    if (j < last) {
-      float v[P::kN];
-      P::widen(*reinterpret_cast<const uint4*>(x.base + x.head * P::kSize + (int64_t)j * 16), v);
+  auto load = [&](int j) { return *reinterpret_cast<const uint4*>(x.base + x.head * P::kSize + (int64_t)j * 16); };
+  auto each = [&](int j, const uint4& p, auto&& f) {
+    float v[P::kN];
+    P::widen(p, v);
 #pragma unroll
-      for (int e = 0; e < P::kN; ++e) offer(v[e], x.head + j * P::kN + e);
-    }
+    for (int e = 0; e < P::kN; ++e) f(v[e], x.head + j * P::kN + e);
+  };
+  // (in any order: the keys are all different)
+  const int work = s.selected * per;
+  for (int q = t; q < work; q += THREADS) {
+    const int from = q / per, j = piece(s.slots[from], q - from * per);
+    if (j >= 0) each(j, load(j), offer);
   }
   if (edge >= 0) offer(P::load(x.base, edge), edge);
   __syncthreads();
@@ -183,12 +205,7 @@ __device__ __forceinline__ void select_top(Selection<THREADS>& s, const Row<F32>
       const Key o = key_of(v, (uint32_t)index);
       best = o < before && o > best ? o : best;
     };
-    for (int j = first + t; j < last; j += THREADS) {
-      float v[P::kN];
-      P::widen(*reinterpret_cast<const uint4*>(x.base + x.head * P::kSize + (int64_t)j * 16), v);
-#pragma unroll
-      for (int e = 0; e < P::kN; ++e) meet(v[e], x.head + j * P::kN + e);
-    }
+    for (int j = t; j < x.full; j += THREADS) each(j, load(j), meet);
     if (edge >= 0) meet(P::load(x.base, edge), edge);
     best = wave_max_key(best);
     if (lane == 0) s.wave_keys[t >> 6] = best;
@@ -227,7 +244,7 @@ __device__ __forceinline__ Sums own_sums(const Row<F32>& x, int first, int last,
 template <bool F32, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void top_row_kernel(TopArgs a) {
   constexpr int W = THREADS / 64;
-  __shared__ Selection<THREADS> selection;
+  __shared__ Selection<THREADS, THREADS> selection;
   __shared__ Sums parts[W];
   const int t = threadIdx.x;
   const int64_t row = blockIdx.x, token = a.tokens[row];
@@ -240,7 +257,12 @@ __global__ __launch_bounds__(THREADS) void top_row_kernel(TopArgs a) {
   const float most = sums.m;
   sums = wave_join(sums, c);
   if ((t & 63) == 0) parts[t >> 6] = sums;
-  select_top<F32, THREADS>(selection, x, 0, x.full, edge, most, a.k);
+  const float bound = bound_of(selection, most, a.k);
+  select_slot(selection, t, most, bound);
+  select_top(selection, x, edge, bound, a.k, (x.full + THREADS - 1) / THREADS, [&](int slot, int i) {
+    const int j = slot + i * THREADS;
+    return j < x.full ? j : -1;
+  });
   sums = wave_join<W>(parts[t & (W - 1)], c);
   if (t < 64) {
     const LogProb lp(sums, c);
@@ -250,22 +272,23 @@ __global__ __launch_bounds__(THREADS) void top_row_kernel(TopArgs a) {
 }
 
 // Few rows: workgroup (part, row) takes the pieces j with j / per == part, and part 0 the row's
-// edges; a second kernel joins the parts' sums and their k largest.
+// edges, and leaves sums and the maxima of 64 slots, the pieces and threads with equal t % 64;
+// a second kernel joins the sums and selects.
 constexpr int kSplitThreads = 256;
 
 // The workspace: the parts' sums and the token's logit, [T][kLossParts] of four floats, then
-// the parts' keys, [T][kLossParts][k].
+// the slots' maxima, [T][kLossParts][64].
 __device__ __forceinline__ float4* part_sums(const TopArgs& a, int64_t row) {
   return reinterpret_cast<float4*>(a.workspace) + row * kLossParts;
 }
-__device__ __forceinline__ Key* part_keys(const TopArgs& a, int64_t row) {
-  return reinterpret_cast<Key*>(a.workspace + a.T * kLossParts * 16) + row * kLossParts * a.k;
+__device__ __forceinline__ float* part_maxima(const TopArgs& a, int64_t row) {
+  return reinterpret_cast<float*>(a.workspace + a.T * kLossParts * 16) + row * kLossParts * 64;
 }
 
 template <bool F32>
 __global__ __launch_bounds__(kSplitThreads) void top_part_kernel(TopArgs a, int per) {
   constexpr int W = kSplitThreads / 64;
-  __shared__ Selection<kSplitThreads> selection;
+  __shared__ float maxima[kSplitThreads];
   __shared__ Sums parts[W];
   const int t = threadIdx.x;
   const int64_t part = blockIdx.x, row = blockIdx.y, token = a.tokens[row];
@@ -275,50 +298,53 @@ __global__ __launch_bounds__(kSplitThreads) void top_part_kernel(TopArgs a, int 
   const int first = (int)part * per, last = first + per < x.full ? first + per : x.full;
   const int edge = part == 0 ? x.edge(t) : -1;
   Sums sums = own_sums<F32, kSplitThreads, 8>(x, first, last, edge, c);
-  const float most = sums.m;
+  maxima[t] = sums.m;
   sums = wave_join(sums, c);
   if ((t & 63) == 0) parts[t >> 6] = sums;
-  select_top<F32, kSplitThreads>(selection, x, first, last, edge, most, a.k);
+  __syncthreads();
+  if (t >= 64) return;
+  float most = maxima[t];
+#pragma unroll
+  for (int w = 1; w < W; ++w) most = fmaxf(most, maxima[w * 64 + t]);
+  part_maxima(a, row)[part * 64 + t] = most;
   sums = wave_join<W>(parts[t & (W - 1)], c);
   if (t == 0)
     part_sums(a, row)[part] = make_float4(sums.m, sums.s, sums.q, part == 0 ? Piece<F32>::load(x.base, token) : 0.0f);
-  if (t < a.k) part_keys(a, row)[part * a.k + t] = selection.keys[t];
 }
 
-// A row's parts: every part's k-th key is at most the row's k-th, so the keys below the largest
-// of those are out; the others are ranked by counting.
-__global__ __launch_bounds__(kSplitThreads) void top_join_kernel(TopArgs a, int parts) {
-  __shared__ Key keys[kLossParts * kTopMost], out[kTopMost];
-  __shared__ int left;
+template <bool F32>
+__global__ __launch_bounds__(kSplitThreads) void top_join_kernel(TopArgs a, int per, int parts) {
+  constexpr int kSlots = kLossParts * 64, kMine = kSlots / kSplitThreads;
+  __shared__ Selection<kSplitThreads, kSlots> selection;
   const int t = threadIdx.x, lane = t & 63;
   const int64_t row = blockIdx.x;
-  if (!in_vocabulary(a, a.tokens[row])) return put_nothing<kSplitThreads>(a, row);
+  // (the loads go out together with the token's; a row that is not read has left nothing here)
+  const int64_t token = a.tokens[row];
   const float c = a.inv_temperature * kLog2e;
+  const Row<F32> x(a.logits, a.ld, row, a.V);
+  const float* const maxima = part_maxima(a, row);
+  float own[kMine], most = kNegInf;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    own[i] = t + i * kSplitThreads < parts * 64 ? maxima[t + i * kSplitThreads] : kNegInf;
+    most = fmaxf(most, own[i]);
+  }
   float4 p = make_float4(kNegInf, 0.0f, 0.0f, 0.0f);
   if (lane < parts) p = part_sums(a, row)[lane];
-  const Sums sums = wave_join(Sums{p.x, p.y, p.z}, c);
   const float mine = part_sums(a, row)[0].w;
-  const Key* const from = part_keys(a, row);
-  const Key bound = wave_max_key(lane < parts ? from[lane * a.k + a.k - 1] : 0);
-  if (t == 0) left = 0;
-  if (t < a.k) out[t] = 0;
-  __syncthreads();
-  for (int i = t; i < parts * a.k; i += kSplitThreads) {
-    const Key k = from[i];
-    if (k && k >= bound) keys[__hip_atomic_fetch_add(&left, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)] = k;
-  }
-  __syncthreads();
-  const int n = left;
-  for (int i = t; i < n; i += kSplitThreads) {
-    const Key k = keys[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += keys[j] > k ? 1 : 0;
-    if (rank < a.k) out[rank] = k;
-  }
-  __syncthreads();
+  if (!in_vocabulary(a, token)) return put_nothing<kSplitThreads>(a, row);
+  const float bound = bound_of(selection, most, a.k);
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) select_slot(selection, t + i * kSplitThreads, own[i], bound);
+  select_top(selection, x, x.edge(t), bound, a.k, (per + 63) / 64, [&](int slot, int i) {
+    const int first = (slot >> 6) * per, last = first + per < x.full ? first + per : x.full;
+    const int j = first + (slot & 63) + i * 64;
+    return j < last ? j : -1;
+  });
   if (t < 64) {
+    const Sums sums = wave_join(Sums{p.x, p.y, p.z}, c);
     const LogProb lp(sums, c);
-    if (t < a.k) put_alternative(a, row, t, out[t], lp);
+    if (t < a.k) put_alternative(a, row, t, selection.keys[t], lp);
     if (t == 0) put_token(a, row, sums, mine);
   }
 }
@@ -348,7 +374,7 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
     top_part_kernel<F32><<<dim3((unsigned)parts, (unsigned)a.T), kSplitThreads, 0, s>>>(a, per);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    top_join_kernel<<<dim3((unsigned)a.T), kSplitThreads, 0, s>>>(a, parts);
+    top_join_kernel<F32><<<dim3((unsigned)a.T), kSplitThreads, 0, s>>>(a, per, parts);
     return hipGetLastError();
   }
   const dim3 grid((unsigned)a.T);
@@ -365,8 +391,8 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
 
 using namespace top_detail;
 
-int64_t top_logprobs_workspace(int64_t T, int64_t V, int64_t k) {
-  return split_rows(T, V) ? T * kLossParts * (16 + 8 * k) : 0;
+int64_t top_logprobs_workspace(int64_t T, int64_t V) {
+  return split_rows(T, V) ? T * kLossParts * (16 + 4 * 64) : 0;
 }
 
 hipError_t launch_top_logprobs(const TopArgs& a, hipStream_t s) {
