@@ -57,8 +57,18 @@ __global__ __launch_bounds__(512) void gemm_mx4_large_kernel(GemmArgs g, int ful
 namespace {
 
 // The kernel of a product of K bytes a row: that of FP8 codes with power-of-two scales, whose
-// steps of 128 bytes of a row these are.
-inline GemmRoute mx4_route(const GemmSize& s) { return gemm_route(kPairBlockE8, s); }
+// steps of 128 bytes of a row these are, but for two kinds of sizes where half an
+// instruction's time shows: large tiles also where they fill whole rounds of the CUs (4096 x 512 x 4096 12.2
+// us, 128 x 128 tiles 13.5; 16384 x 512 x 12288 116 and 123), and up to two 64 x 64 tiles a CU before
+// 128 x 128 tiles of eight waves, but for a single row of them (512 x 4096 x 4096 9.1 us, eight waves
+// 11.8; 512 x 12288 x 4096 27.8 and 31.1; 192 x 1024 x 8192 4.9 and 5.8; 64 x 5120 x 17408 23.1 and 21.1).
+// Over 110 sizes, half of them random, the choice is about 1% above the best of these kernels.
+inline GemmRoute mx4_route(const GemmSize& s) {
+  const GemmRoute r = gemm_route(kPairBlockE8, s);
+  if (r == kMidTiles && tile_count(s, 256, 256) % kCUs == 0) return kLargeTiles;
+  if (r == kEightWaves && s.M > 64 && tile_count(s, 64, 64) <= 2 * kCUs) return kSmallTiles;
+  return r;
+}
 
 template <int BM, int BN, int WM, int WN, int KS = 1>
 hipError_t launch_mx4_tiles(const GemmArgs& g, hipStream_t s) {
