@@ -134,18 +134,22 @@ __device__ __forceinline__ uint32_t key_of(int64_t token, int64_t V) {
   return token >= 0 && token < V ? (uint32_t)token : (uint32_t)V;
 }
 
-// Which tokens occur: bit v / 8 of part v % 8, parts of used_words(V) words.
-constexpr int kClasses = 8;
+// Which tokens occur: bit v / kClasses of part v % kClasses, parts of used_words(V) words.
+constexpr int kClassBits = 6, kClasses = 1 << kClassBits;
 __host__ __device__ constexpr int64_t used_words(int64_t V) { return (V + 32 * kClasses - 1) / (32 * kClasses); }
+__device__ __forceinline__ bool occurs(const uint32_t* used, int64_t V, uint64_t v) {
+  return used[(v & (kClasses - 1)) * used_words(V) + (v >> (kClassBits + 5))] >> (v >> kClassBits & 31) & 1;
+}
 
-// Up to kSortMost tokens: workgroup g takes those with token % 8 = g out of all and sorts them by
-// token / 8, its place in the whole being after those of the workgroups before it (equal
-// tokens stay together, which is all that the sums ask for; 16384 tokens with frequencies of 1 / rank in one
-// workgroup 25 us).  Tokens outside the vocabulary are the last of the last class.  A word holds
+// Up to kSortMost tokens: workgroup g takes those with token % kClasses = g out of all and sorts
+// them by token / kClasses, its place in the whole being after those of the workgroups before it
+// (equal tokens stay together, which is all that the sums ask for).  16384 tokens with frequencies of 1 /
+// rank in one workgroup 25 us, in eight 19, here 17.  Tokens outside the vocabulary are the
+// last of the last class.  A word holds
 // key and t together (kPosBits for t), so the pass that a key makes is one word through LDS.  Wave w has the words
 // from w 64 rounds on, so that its rounds go in order.
 constexpr int kSortThreads = 1024, kSortWaves = 16, kSortRounds = 16, kPosBits = 14;
-constexpr int64_t kSortMost = 16384, kSortMostV = ((int64_t)1 << (32 - kPosBits + 3)) - 16;
+constexpr int64_t kSortMost = 16384, kSortMostV = ((int64_t)1 << (32 - kPosBits + kClassBits)) - 2 * kClasses;
 constexpr int kDigit = 9;  // bits a pass, at most
 constexpr int kUsedLds = 1024;  // words of a part of the bitmap in LDS
 
@@ -159,7 +163,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int64_t*
   const uint32_t g = blockIdx.x;
   uint32_t w[kSortRounds], rank[kSortRounds];
   int rounds = (T + kSortThreads - 1) / kSortThreads, first = wave * rounds * 64 + lane;
-  const uint32_t outside = (uint32_t)((V + 7) / 8 * 8 + 7);
+  const uint32_t outside = (uint32_t)((V + kClasses - 1) / kClasses * kClasses + kClasses - 1);
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
     const int i = first + r * 64;
@@ -173,8 +177,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int64_t*
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
     const bool live = r < rounds && first + r * 64 < T;
-    own += (uint32_t)__popcll(__ballot(live && (rank[r] & 7) == g));
-    less += (uint32_t)__popcll(__ballot(live && (rank[r] & 7) < g));
+    own += (uint32_t)__popcll(__ballot(live && (rank[r] & (kClasses - 1)) == g));
+    less += (uint32_t)__popcll(__ballot(live && (rank[r] & (kClasses - 1)) < g));
   }
   if (lane == 0) {
     sums[wave] = own;
@@ -190,11 +194,11 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int64_t*
   }
 #pragma unroll
   for (int r = 0; r < kSortRounds; ++r) {
-    const bool mine = r < rounds && first + r * 64 < T && (rank[r] & 7) == g;
+    const bool mine = r < rounds && first + r * 64 < T && (rank[r] & (kClasses - 1)) == g;
     const uint64_t m = __ballot(mine);
     if (mine)
       words[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] =
-          rank[r] >> 3 << kPosBits | (uint32_t)(first + r * 64);
+          rank[r] >> kClassBits << kPosBits | (uint32_t)(first + r * 64);
     at += (uint32_t)__popcll(m);
   }
   __syncthreads();
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int64_t*
   for (int r = 0; r < kSortRounds; ++r) {
     const int i = first + r * 64;
     if (r < rounds && i < n) {
-      const uint32_t high = w[r] >> kPosBits, key = high << 3 | g;
+      const uint32_t high = w[r] >> kPosBits, key = high << kClassBits | g;
       keys[place + i] = key;
       positions[place + i] = w[r] & ((1u << kPosBits) - 1);
       if (key < (uint32_t)V)
@@ -375,8 +379,8 @@ __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(SortPass p) {
     p.keys_out[to] = key[r];
     p.positions_out[to] = p.tokens ? (uint32_t)i : p.positions[i];
     if (p.used && key[r] < (uint32_t)p.V) {
-      const uint32_t high = key[r] >> 3;
-      __hip_atomic_fetch_or(p.used + (key[r] & 7) * used_words(p.V) + (high >> 5), 1u << (high & 31), __ATOMIC_RELAXED,
+      const uint32_t high = key[r] >> kClassBits;
+      __hip_atomic_fetch_or(p.used + (key[r] & (kClasses - 1)) * used_words(p.V) + (high >> 5), 1u << (high & 31), __ATOMIC_RELAXED,
                             __HIP_MEMORY_SCOPE_AGENT);
     }
   }
@@ -425,7 +429,7 @@ __global__ __launch_bounds__(kThreads) void embedding_fill_kernel(Gradient g) {
   v += more;
   c -= (int64_t)more * g.row.d;
   if (v >= (uint64_t)a.V) return;
-  if (g.used[(v & 7) * used_words(a.V) + (v >> 8)] >> (v >> 3 & 31) & 1) return;
+  if (occurs(g.used, a.V, v)) return;
   const int64_t at = (int64_t)v * a.ldw + c * kN;
   const v4u zero = {0, 0, 0, 0};
   if constexpr (F32)
@@ -574,7 +578,7 @@ __global__ __launch_bounds__(kThreads) void embedding_join_kernel(Gradient g) {
   };
   Eight sum = load(part + a.C), old{};
   if (ADD) old = load_row<F32>(a, key, c, second);
-  constexpr int kAhead = 8;
+  constexpr int kAhead = 16;
   for (int i0 = 1; i0 <= more; i0 += kAhead) {
     Eight x[kAhead];
 #pragma unroll
@@ -652,7 +656,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t
   int out = 0;
   hipError_t e;
   if (l.small) {
-    sort_small_kernel<<<kClasses, kSortThreads, 0, s>>>(a.tokens, (int)a.T, a.V, bits_of((a.V + 7) / 8),
+    sort_small_kernel<<<kClasses, kSortThreads, 0, s>>>(a.tokens, (int)a.T, a.V, bits_of((a.V + kClasses - 1) / kClasses),
                                                         words(l.keys[0]), words(l.positions[0]), words(l.used));
     if ((e = hipGetLastError()) != hipSuccess) return e;
   } else {
