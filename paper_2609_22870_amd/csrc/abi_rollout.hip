@@ -143,8 +143,8 @@ fp8q_status fp8q_embedding(const void* weight, fp8q_dtype dtype, int64_t V, int6
 
 int64_t fp8q_embedding_backward_workspace(int64_t T, int64_t V, int64_t C) {
   if (T <= 0 || V <= 0 || C <= 0 || T > kMaxRows || !dims_ok(V, C) || C % 16 || V * C >= ((int64_t)1 << 33)) return -1;
-  // workgroups of the sums, chunks of eight tokens or more by bands of 2048 columns, beside those
-  // that fill, of 256 pieces of 16 bytes: less than 2^32 threads together
+  // (launches of less than 2^32 threads: a thread of the zeros 16 bytes, a workgroup of the sums eight
+  // tokens or more by a band of 2048 columns)
   if (T * ((C + 2047) / 2048) > ((int64_t)1 << 25)) return -1;
   return fp8q::embedding_backward_workspace(T, V, C);
 }
