@@ -1378,7 +1378,7 @@ __device__ __forceinline__ void thin_tile(const GemmArgs& g, uint8_t* lds, int t
   constexpr bool kMx = PAIR == kPairMx4;
   constexpr bool kBlockScaled = PAIR == kPairBlock || PAIR == kPairBlockK || PAIR == kPairBlockE8;
   constexpr bool kWeightBlocks = PAIR == kPairBlock || PAIR == kPairBlockE8;
-  static_assert(TJ <= 8 && 8 % TJ == 0, "a tile's columns lie in one 128-column weight block");
+  static_assert(TJ <= 8 && (kMx || 8 % TJ == 0), "a tile's columns lie in one 128-column weight block");
   static_assert(!GATED || (PAIR == kPairBlock && !QOUT && TJ % 2 == 0), "gated: as many columns of both weights");
   constexpr int W = kThinWaves, kColScales = GATED ? 2 : (kWeightBlocks ? 1 : TJ * 4);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);

@@ -183,3 +183,13 @@ def test_layer_of_ragged_width():
     ref, absum = vx @ vw.t(), vx.abs() @ vw.abs().t()
     f = (9 * 8 + 9) * 2.0 ** -23
     within(c, ref, f * absum + bf16_half(ref.abs() + f * absum), "ragged layer")
+
+
+@pytest.mark.parametrize("M,N,K", [(64, 5120, 2816), (49, 5076, 4352), (100, 5220, 9984), (250, 2300, 13056)])
+def test_three_strips(M, N, K):
+    """Thin tiles of 48 columns."""
+    assert route(M, N, K) == 5
+    print("mx4 product", M, N, K, flush=True)
+    a, b = operand(M, K, 21), operand(N, K, 22)
+    c = check_product(a, b, M, N, K, (M, N, K))
+    same(c, fp8q.gemm_mx4(a[2], a[3], b[2], b[3]), "two runs")
