@@ -11,9 +11,9 @@
 // leaves a sum per chunk in the workspace, and a second kernel adds those in order.  The rows of
 // tokens that do not occur are filled with zeros by a launch between the sort, which leaves a bitmap of
 // those that do, and the sums: most of what a whole gradient costs.  Bound by HBM, V C elements written
-// and T C read: 16384 tokens, 131072 x 4096 fp32 422 us, of them the sort 17, zeros 300 (6.7 TB/s), sums
-// 98 and their join 7.  Small tables wait for the chain of launches: 5003 tokens, 32000 x 2048 bf16, twice,
-// about 80 us where the bytes would take 33.
+// and T C read: 16384 tokens, 131072 x 4096 fp32 422 us, of them the sort 14, zeros 300 (7.1 TB/s), sums
+// 98 and their join 7.  Small tables wait for the chain of launches: 5003 tokens, 32000 x 2048 bf16, twice, 89
+// us (sorts 7, zeros 18, sums 10 and 14, joins 8) where the bytes would take 33.
 #include "device_common.h"
 #include "rollout.h"
 
@@ -146,82 +146,54 @@ __device__ __forceinline__ bool occurs(const uint32_t* used, int64_t V, uint64_t
 // Up to kSortMost tokens: workgroup g takes those with token % kClasses = g out of all and sorts
 // them by token / kClasses, its place in the whole being after those of the workgroups before it
 // (equal tokens stay together, which is all that the sums ask for).  16384 tokens with frequencies of 1 /
-// rank in one workgroup 25 us, in eight 19, here 17.  Tokens outside the vocabulary are the
+// rank in one workgroup 25 us, in eight 19, in 64 17 (before what is said below).  Tokens outside the vocabulary are the
 // last of the last class.  A word holds
 // key and t together (kPosBits for t), so the pass that a key makes is one word through LDS.  Wave w has the words
 // from w 64 rounds on, so that its rounds go in order.
-constexpr int kSortThreads = 1024, kSortWaves = 16, kSortRounds = 16, kPosBits = 14;
+//
+// What it waits for is its own chain, and of that much is code that is met for the first time: a chain of rounds that
+// are skipped costs as much as one that works.  So the kernel has as many rounds as T asks for, 4, 8 or 16, and
+// sorts in two where its class has no more keys than that (5003 tokens 6.6 us, with 16 rounds throughout 11.0;
+// 16384 13.9 and 16.6).
+constexpr int kSortThreads = 1024, kSortWaves = 16, kSortRounds = 16, kFewRounds = 2, kPosBits = 14;
 constexpr int64_t kSortMost = 16384;
 constexpr int kDigit = 9;  // bits a pass, at most
 constexpr int kUsedLds = 1024;  // words of a part of the bitmap in LDS
 static_assert(kUsedLds * 32 < 1 << (32 - kPosBits));  // (their keys, and that of the tokens outside, fit beside t)
 
-__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int64_t* tokens, int T, int64_t V, int key_bits,
-                                                                  uint32_t* keys, uint32_t* positions,
-                                                                  uint32_t* used) {
-  __shared__ uint32_t words[kSortMost];
-  __shared__ uint32_t counters[kSortWaves][1 << kDigit], sums[kSortWaves], lower[kSortWaves];
-  __shared__ uint32_t marks[kUsedLds];
+struct SmallSort {
+  uint32_t words[kSortMost];
+  uint32_t counters[kSortWaves][1 << kDigit], sums[kSortWaves], lower[kSortWaves];
+  uint32_t marks[kUsedLds];
+};
+
+struct SmallSortArgs {
+  const int64_t* tokens;
+  int T, key_bits;
+  int64_t V;
+  uint32_t *keys, *positions, *used;
+};
+
+// The class's n words, of up to ROUNDS rounds, sorted in LDS and written from `place` on.
+template <int ROUNDS>
+__device__ __forceinline__ void sort_class(SmallSort& s, const SmallSortArgs& a, int n, uint32_t place) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const uint32_t g = blockIdx.x;
-  uint32_t w[kSortRounds], rank[kSortRounds];
-  int rounds = (T + kSortThreads - 1) / kSortThreads, first = wave * rounds * 64 + lane;
-  const uint32_t outside = (uint32_t)((V + kClasses - 1) / kClasses * kClasses + kClasses - 1);
+  const int rounds = (n + kSortThreads - 1) / kSortThreads, first = wave * rounds * 64 + lane;
+  uint32_t w[ROUNDS], rank[ROUNDS];
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
-    const int i = first + r * 64;
-    int64_t token = 0;
-    if (r < rounds && i < T) token = tokens[i];
-    rank[r] = token >= 0 && token < V ? (uint32_t)token : outside;
-  }
-  for (int64_t i = t; i < kUsedLds; i += kSortThreads) marks[i] = 0;
-  // this class's words, in order
-  uint32_t own = 0, less = 0;
-#pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
-    const bool live = r < rounds && first + r * 64 < T;
-    own += (uint32_t)__popcll(__ballot(live && (rank[r] & (kClasses - 1)) == g));
-    less += (uint32_t)__popcll(__ballot(live && (rank[r] & (kClasses - 1)) < g));
-  }
-  if (lane == 0) {
-    sums[wave] = own;
-    lower[wave] = less;
-  }
-  __syncthreads();
-  uint32_t at = 0, place = 0, count = 0;
-#pragma unroll
-  for (int o = 0; o < kSortWaves; ++o) {
-    at += o < wave ? sums[o] : 0;
-    count += sums[o];
-    place += lower[o];
-  }
-#pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
-    const bool mine = r < rounds && first + r * 64 < T && (rank[r] & (kClasses - 1)) == g;
-    const uint64_t m = __ballot(mine);
-    if (mine)
-      words[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] =
-          rank[r] >> kClassBits << kPosBits | (uint32_t)(first + r * 64);
-    at += (uint32_t)__popcll(m);
-  }
-  __syncthreads();
-  const int n = (int)count;
-  rounds = (n + kSortThreads - 1) / kSortThreads;
-  first = wave * rounds * 64 + lane;
-#pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     w[r] = 0xffffffffu;
-    if (r < rounds && first + r * 64 < n) w[r] = words[first + r * 64];
+    if (r < rounds && first + r * 64 < n) w[r] = s.words[first + r * 64];
   }
-  const int passes = (key_bits + kDigit - 1) / kDigit, bits = (key_bits + passes - 1) / passes;
-  uint32_t* const mine = counters[wave];
+  const int passes = (a.key_bits + kDigit - 1) / kDigit, bits = (a.key_bits + passes - 1) / passes;
+  uint32_t* const mine = s.counters[wave];
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = kPosBits + pass * bits;
     auto digit_of = [&](uint32_t x) { return x >> shift & ((1u << bits) - 1); };
     for (int d = lane; d < 1 << kDigit; d += 64) mine[d] = 0;
     in_order();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r)
+    for (int r = 0; r < ROUNDS; ++r)
       if (r < rounds) rank[r] = rank_in_wave<kDigit>(digit_of(w[r]), first + r * 64 < n, mine);
     __syncthreads();
     // prefix sums over the digits, and over the waves of a digit: two threads a digit
@@ -230,7 +202,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int64_t*
     uint32_t c[kPer], sum = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      c[i] = counters[(t & 1) * kPer + i][t >> 1];
+      c[i] = s.counters[(t & 1) * kPer + i][t >> 1];
       sum += c[i];
     }
     uint32_t scan = sum;
@@ -239,40 +211,94 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(const int64_t*
       const uint32_t o = __shfl_up(scan, d, 64);
       if (lane >= d) scan += o;
     }
-    if (lane == 63) sums[wave] = scan;
+    if (lane == 63) s.sums[wave] = scan;
     __syncthreads();
     uint32_t base = scan - sum;
 #pragma unroll
-    for (int o = 0; o < kSortWaves; ++o) base += o < wave ? sums[o] : 0;
+    for (int o = 0; o < kSortWaves; ++o) base += o < wave ? s.sums[o] : 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      counters[(t & 1) * kPer + i][t >> 1] = base;
+      s.counters[(t & 1) * kPer + i][t >> 1] = base;
       base += c[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r)
-      if (r < rounds && first + r * 64 < n) words[mine[digit_of(w[r])] + rank[r]] = w[r];
+    for (int r = 0; r < ROUNDS; ++r)
+      if (r < rounds && first + r * 64 < n) s.words[mine[digit_of(w[r])] + rank[r]] = w[r];
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r)
-      if (r < rounds && first + r * 64 < n) w[r] = words[first + r * 64];
+    for (int r = 0; r < ROUNDS; ++r)
+      if (r < rounds && first + r * 64 < n) w[r] = s.words[first + r * 64];
     // (the next pass writes the words again only after more barriers)
   }
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     const int i = first + r * 64;
     if (r < rounds && i < n) {
-      const uint32_t high = w[r] >> kPosBits, key = high << kClassBits | g;
-      keys[place + i] = key;
-      positions[place + i] = w[r] & ((1u << kPosBits) - 1);
-      if (key < (uint32_t)V)
-        __hip_atomic_fetch_or(marks + (high >> 5), 1u << (high & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      const uint32_t high = w[r] >> kPosBits, key = high << kClassBits | blockIdx.x;
+      a.keys[place + i] = key;
+      a.positions[place + i] = w[r] & ((1u << kPosBits) - 1);
+      if (key < (uint32_t)a.V)
+        __hip_atomic_fetch_or(s.marks + (high >> 5), 1u << (high & 31), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
   }
+}
+
+template <int ROUNDS>
+__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(SmallSortArgs a) {
+  __shared__ SmallSort s;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const uint32_t g = blockIdx.x;
+  uint32_t key[ROUNDS];
+  const int rounds = (a.T + kSortThreads - 1) / kSortThreads, first = wave * rounds * 64 + lane;
+  const uint32_t outside = (uint32_t)((a.V + kClasses - 1) / kClasses * kClasses + kClasses - 1);
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int i = first + r * 64;
+    int64_t token = 0;
+    if (r < rounds && i < a.T) token = a.tokens[i];
+    key[r] = token >= 0 && token < a.V ? (uint32_t)token : outside;
+  }
+  s.marks[t] = 0;
+  static_assert(kUsedLds == kSortThreads);
+  // this class's words, in order
+  uint32_t own = 0, less = 0;
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const bool live = r < rounds && first + r * 64 < a.T;
+    own += (uint32_t)__popcll(__ballot(live && (key[r] & (kClasses - 1)) == g));
+    less += (uint32_t)__popcll(__ballot(live && (key[r] & (kClasses - 1)) < g));
+  }
+  if (lane == 0) {
+    s.sums[wave] = own;
+    s.lower[wave] = less;
+  }
   __syncthreads();
-  const int64_t part = used_words(V);
-  for (int64_t i = t; i < part; i += kSortThreads) used[g * part + i] = marks[i];
+  uint32_t at = 0, place = 0, count = 0;
+#pragma unroll
+  for (int o = 0; o < kSortWaves; ++o) {
+    at += o < wave ? s.sums[o] : 0;
+    count += s.sums[o];
+    place += s.lower[o];
+  }
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const bool mine = r < rounds && first + r * 64 < a.T && (key[r] & (kClasses - 1)) == g;
+    const uint64_t m = __ballot(mine);
+    if (mine)
+      s.words[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0))] =
+          key[r] >> kClassBits << kPosBits | (uint32_t)(first + r * 64);
+    at += (uint32_t)__popcll(m);
+  }
+  __syncthreads();
+  const int n = __builtin_amdgcn_readfirstlane((int)count);
+  if (n <= kFewRounds * kSortThreads)
+    sort_class<kFewRounds>(s, a, n, place);
+  else
+    sort_class<ROUNDS>(s, a, n, place);
+  __syncthreads();
+  const int64_t part = used_words(a.V);
+  if (t < part) a.used[g * part + t] = s.marks[t];
 }
 
 // More tokens: tiles of kTile in a workgroup each, a pass being three launches (the tiles'
@@ -659,8 +685,14 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t
   int out = 0;
   hipError_t e;
   if (l.small) {
-    sort_small_kernel<<<kClasses, kSortThreads, 0, s>>>(a.tokens, (int)a.T, a.V, bits_of((a.V + kClasses - 1) / kClasses),
-                                                        words(l.keys[0]), words(l.positions[0]), words(l.used));
+    const SmallSortArgs p{a.tokens, (int)a.T, bits_of((a.V + kClasses - 1) / kClasses), a.V,
+                          words(l.keys[0]), words(l.positions[0]), words(l.used)};
+    if (a.T <= 4 * kSortThreads)
+      sort_small_kernel<4><<<kClasses, kSortThreads, 0, s>>>(p);
+    else if (a.T <= 8 * kSortThreads)
+      sort_small_kernel<8><<<kClasses, kSortThreads, 0, s>>>(p);
+    else
+      sort_small_kernel<kSortRounds><<<kClasses, kSortThreads, 0, s>>>(p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   } else {
     const int bits = bits_of(a.V);
