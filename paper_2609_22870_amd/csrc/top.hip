@@ -221,6 +221,9 @@ __device__ __forceinline__ void select_top(Selection<THREADS, SLOTS>& s, const R
 }
 
 // The sums of pieces first + t + i THREADS below last and of this thread's edge; NV in flight.
+// Chunks that are nothing but padding for the whole workgroup are left out (64 x 131072 bf16 15.1
+// -> 13.5 us, 2048 x 8000 fp32 22.2 -> 20.0; where none is, up to 2% for the test; workgroups of 1024 have rows
+// that fill them and lost as much).
 template <bool F32, int THREADS, int NV>
 __device__ __forceinline__ Sums own_sums(const Row<F32>& x, int first, int last, int edge, float c) {
   using P = Piece<F32>;
@@ -232,6 +235,7 @@ __device__ __forceinline__ Sums own_sums(const Row<F32>& x, int first, int last,
     for (int i = 0; i < NV; ++i) held[i] = x.piece(j0 + i * THREADS, last, threadIdx.x);
 #pragma unroll
     for (int i = 0; i < NV; i += kChunk) {
+      if (THREADS < 1024 && j0 + i * THREADS >= last) break;
       add_pieces<F32, kChunk>(held + i, c, sums);
       __builtin_amdgcn_sched_barrier(0);
     }
