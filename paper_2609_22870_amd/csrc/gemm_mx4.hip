@@ -3,6 +3,11 @@
 // fp32 accumulation inside the matrix instruction, which applies the scales, bf16 output.
 // The kernels are those of gemm_tile.h: a K step is the 128 bytes that an FP8 step is, but
 // 256 codes, two instructions of half an FP8 one's time.
+//
+// Large products are bound by power: 16384 x 4096 x 12288 385 us, 4.3 PFLOP/s, at a clock of 1.63 to 1.66
+// GHz (operands of zeros 322; the matrix instructions alone reach 8.3 PFLOP/s).  Few rows are bound
+// by the bytes that a CU loads, about 85 KB a us: 8 x 4096 x 12288 6.0 us (4.5 TB/s of weights), 64 x
+// 17408 x 5120 13.4 (3.7 TB/s).
 #include "gemm_tile.h"
 #include "rollout.h"
 

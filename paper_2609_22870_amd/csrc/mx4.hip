@@ -10,7 +10,8 @@
 // 13.2%.)  x / S is exact, so a code is rounded once.  A unit that holds a NaN or an infinity gets the
 // byte 255, E8M0's NaN, which a product and the values carry on.
 //
-// Bound by HBM: 2 bytes read and 17/32 written an element.
+// Bound by HBM: 2 bytes read and 17/32 written an element, the other way round for the values
+// (12288 x 4096: codes 22.3 us, 5.7 TB/s, values 21.2, 6.0).
 #include "device_common.h"
 #include "rollout.h"
 
