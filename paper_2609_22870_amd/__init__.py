@@ -894,7 +894,8 @@ def dequantize_mx4(codes, scales, cols=None, out=None):
 def gemm_mx4(a, sa, b, sb, out=None):
     """bf16 out[M, N] = A B^T of MXFP4 operands as quantize_mx4() gives them: a, sa the codes
     [M, K / 2] and scales of the activations, b, sb those of a weight stored [N, K]; fp32
-    accumulation."""
+    accumulation.  Rows of out lie a multiple of 4 elements apart: a new one of another N has
+    room behind each row."""
     r = _fast().gemm_mx4(a, sa, b, sb, out)
     if r is not None:
         return _done(r, "fp8q_gemm_mx4")
@@ -902,7 +903,9 @@ def gemm_mx4(a, sa, b, sb, out=None):
     N, K2 = _mx4(b, sb, "b", a.device)
     if K != K2:
         raise ValueError("contraction sizes differ")
-    out = _given(out, torch.bfloat16, "out", (M, N), a.device)
+    if out is None:
+        out = torch.empty((M, -(-N // 4) * 4), dtype=torch.bfloat16, device=a.device)[:, :N]
+    _matrix(out, torch.bfloat16, "out", (M, N), a.device)
     st = lib().fp8q_gemm_mx4(a.data_ptr(), sa.data_ptr(), _ld(a), b.data_ptr(), sb.data_ptr(), _ld(b), M, N, K,
                              out.data_ptr(), _ld(out), _stream(a))
     _check(st, "fp8q_gemm_mx4")

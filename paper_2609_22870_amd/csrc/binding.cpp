@@ -806,7 +806,7 @@ PyObject* py_gemm_mx4(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   return guarded<5>(m, a, n, [](const Api& api, PyObject* const* a) -> PyObject* {
     const c10::Device device = tensor(a[0]).device();
     const Mx4 p(a[0], a[1], device), q(a[2], a[3], device);
-    if (p.K != q.K) leave();
+    if (p.K != q.K || (a[4] == Py_None && q.rows % 4)) leave();
     const at::Tensor out = matrix_or_new(a[4], at::kBFloat16, p.rows, q.rows, device);
     void* cp = out.mutable_data_ptr();
     ihipStream_t* s = stream_of(out);

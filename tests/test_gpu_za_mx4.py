@@ -193,3 +193,18 @@ def test_three_strips(M, N, K):
     a, b = operand(M, K, 21), operand(N, K, 22)
     c = check_product(a, b, M, N, K, (M, N, K))
     same(c, fp8q.gemm_mx4(a[2], a[3], b[2], b[3]), "two runs")
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 3, 256), (1, 1001, 4096), (40, 1, 768), (70, 5075, 2816), (500, 701, 1024), (1030, 2050, 256),
+                                   (192, 8189, 256), (2050, 2302, 256), (4090, 4097, 512), (256, 4094, 512), (100, 130, 5376)])
+def test_any_number_of_outputs(M, N, K):
+    """N that is no multiple of 4: a new output has room behind its rows, and nothing is written there."""
+    print("mx4 product", M, N, K, "route", route(M, N, K), flush=True)
+    a, b = operand(M, K, 23), operand(N, K, 24)
+    c = check_product(a, b, M, N, K, (M, N, K))
+    wide = torch.full((M, -(-N // 4) * 4 + 4), 3.0, dtype=torch.bfloat16, device=DEV)
+    same(fp8q.gemm_mx4(a[2], a[3], b[2], b[3], out=wide[:, :N]), c, "given")
+    assert bool((wide[:, N:] == 3.0).all())
+    if N % 4:
+        with pytest.raises(fp8q.Fp8qError):
+            fp8q.gemm_mx4(a[2], a[3], b[2], b[3], out=torch.empty(M, N, dtype=torch.bfloat16, device=DEV))

@@ -102,6 +102,7 @@ def test_other_calls_are_left(path, stub):  # noqa: F811
     q = dict(a=torch.zeros(6, 256, dtype=torch.uint8), s=torch.zeros(96, dtype=torch.uint8))
     assert m.gemm_mx4(q["a"], q["s"][:95], q["a"], q["s"], None) is None           # scales too short
     assert m.gemm_mx4(q["a"], q["s"], q["a"][:, :128], q["s"], None) is None       # K differs
+    assert m.gemm_mx4(q["a"], q["s"], q["a"], q["s"], None) is None                # N = 6: rows with room behind
     assert m.dequantize_mx4(q["a"], q["s"], 513, None) is None
     assert m.dequantize_mx4(q["a"], q["s"], 0, None) is None
     dy, t = torch.zeros(5, 32, dtype=torch.bfloat16), torch.zeros(5, dtype=torch.int64)
