@@ -301,118 +301,125 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(SmallSortArgs 
   if (t < part) a.used[g * part + t] = s.marks[t];
 }
 
-// More tokens: tiles of kTile in a workgroup each, a pass being three launches (the tiles'
-// counts by digit, their prefix sums, the words to their places).  The first pass reads the tokens.
-constexpr int kTileThreads = 256, kTileWaves = 4, kTileRounds = 16, kTile = kTileThreads * kTileRounds;
-constexpr int kWideDigit = 8;
+// More tokens: a workgroup takes a tile of them, up to kTiles tiles, and a pass is two launches, the tiles'
+// counts by digit and the words to their places, where every workgroup adds up the counts before its own.
+// The first pass reads the tokens.  (WIDE_NOW.)
+constexpr int kWideThreads = 512, kWideWaves = 8, kWideDigit = 9, kWideAhead = 4;
+static_assert(kWideThreads == 1 << kWideDigit);  // (thread d has digit d)
+constexpr int64_t kTiles = 128, kTileStep = 2 * kWideThreads;
+
+// Tokens of a tile: whole rounds of every wave.
+inline int64_t tile_of(int64_t T) { return ((T + kTiles - 1) / kTiles + kTileStep - 1) / kTileStep * kTileStep; }
 
 struct SortPass {
   const int64_t* tokens;  // of the first pass, else null
   const uint32_t *keys, *positions;
   uint32_t *keys_out, *positions_out;
-  uint32_t* counts;  // [256][tiles]
+  uint32_t* counts;  // [tiles][512]
   int64_t T, V;
-  int tiles, shift;
-  uint32_t* used;  // of the last pass, else null
+  int tile, tiles, shift;
+  uint32_t* used;  // of the first pass of a whole gradient, else null: cleared
   __device__ __forceinline__ uint32_t key(int64_t i) const { return tokens ? key_of(tokens[i], V) : keys[i]; }
   __device__ __forceinline__ uint32_t digit(uint32_t k) const { return k >> shift & ((1u << kWideDigit) - 1); }
 };
 
-__global__ __launch_bounds__(kTileThreads) void sort_count_kernel(SortPass p) {
+__global__ __launch_bounds__(kWideThreads) void sort_count_kernel(SortPass p) {
   __shared__ uint32_t counts[1 << kWideDigit];
   const int t = threadIdx.x;
   counts[t] = 0;
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * kTile + t;
+  const int64_t first = (int64_t)blockIdx.x * p.tile, last = first + p.tile < p.T ? first + p.tile : p.T;
+  for (int64_t i0 = first + t; i0 < last; i0 += kWideAhead * kWideThreads) {
+    uint32_t key[kWideAhead];
 #pragma unroll
-  for (int r = 0; r < kTileRounds; ++r) {
-    const int64_t i = first + r * kTileThreads;
-    if (i < p.T) __hip_atomic_fetch_add(counts + p.digit(p.key(i)), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    for (int u = 0; u < kWideAhead; ++u) {
+      const int64_t i = i0 + u * kWideThreads;
+      key[u] = i < last ? p.key(i) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kWideAhead; ++u)
+      if (i0 + u * kWideThreads < last)
+        __hip_atomic_fetch_add(counts + p.digit(key[u]), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   }
   __syncthreads();
-  p.counts[(int64_t)t * p.tiles + blockIdx.x] = counts[t];
+  p.counts[(int64_t)blockIdx.x * kWideThreads + t] = counts[t];
   if (p.used)
-    for (int64_t i = (int64_t)blockIdx.x * kTileThreads + t; i < kClasses * used_words(p.V);
-         i += (int64_t)gridDim.x * kTileThreads)
+    for (int64_t i = (int64_t)blockIdx.x * kWideThreads + t; i < kClasses * used_words(p.V);
+         i += (int64_t)gridDim.x * kWideThreads)
       p.used[i] = 0;
 }
 
-// Exclusive prefix sums of n counts, by one workgroup.
-__global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(uint32_t* counts, int64_t n) {
-  __shared__ uint32_t sums[kSortWaves];
-  const int t = threadIdx.x, lane = t & 63;
-  uint32_t carry = 0;
-  constexpr int kPer = 8;
-  for (int64_t first = 0; first < n; first += kSortThreads * kPer) {
-    uint32_t v[kPer], sum = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int64_t at = first + t * kPer + i;
-      v[i] = at < n ? counts[at] : 0;
-      sum += v[i];
-    }
-    uint32_t scan = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint32_t o = __shfl_up(scan, d, 64);
-      if (lane >= d) scan += o;
-    }
-    if (lane == 63) sums[t >> 6] = scan;
-    __syncthreads();
-    uint32_t base = carry + scan - sum, all = 0;
-    for (int w = 0; w < kSortWaves; ++w) {
-      if (w < t >> 6) base += sums[w];
-      all += sums[w];
-    }
-    carry += all;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int64_t at = first + t * kPer + i;
-      if (at < n) counts[at] = base;
-      base += v[i];
-    }
-    __syncthreads();
-  }
-}
-
-__global__ __launch_bounds__(kTileThreads) void sort_move_kernel(SortPass p) {
-  __shared__ uint32_t counters[kTileWaves][1 << kWideDigit];
+__global__ __launch_bounds__(kWideThreads) void sort_move_kernel(SortPass p) {
+  __shared__ uint32_t counters[kWideWaves][1 << kWideDigit], sums[kWideWaves];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int64_t first = (int64_t)blockIdx.x * kTile + wave * (kTileRounds * 64) + lane;
-  for (int d = lane; d < 1 << kWideDigit; d += 64) counters[wave][d] = 0;
-  in_order();
-  uint32_t key[kTileRounds], rank[kTileRounds];
 #pragma unroll
-  for (int r = 0; r < kTileRounds; ++r) {
-    const int64_t i = first + r * 64;
-    key[r] = i < p.T ? p.key(i) : 0;
-  }
-#pragma unroll
-  for (int r = 0; r < kTileRounds; ++r)
-    rank[r] = rank_in_wave<kWideDigit>(p.digit(key[r]), first + r * 64 < p.T, counters[wave]);
+  for (int w = 0; w < kWideWaves; ++w) counters[w][t] = 0;
   __syncthreads();
-  // each digit's waves, in order, after the digit's place for this tile
-  uint32_t base = p.counts[(int64_t)t * p.tiles + blockIdx.x];
+  // this wave's part of the tile
+  const int per = p.tile / kWideWaves;
+  const int64_t first = (int64_t)blockIdx.x * p.tile + wave * per;
+  const int64_t last = first + per < p.T ? first + per : p.T;
+  auto each = [&](auto&& f) {
+    for (int64_t i0 = first; i0 < last; i0 += kWideAhead * 64) {
+      uint32_t key[kWideAhead], position[kWideAhead];
 #pragma unroll
-  for (int w = 0; w < kTileWaves; ++w) {
+      for (int u = 0; u < kWideAhead; ++u) {
+        const int64_t i = i0 + u * 64 + lane;
+        key[u] = i < last ? p.key(i) : 0;
+        position[u] = p.tokens || i >= last ? (uint32_t)i : p.positions[i];
+      }
+#pragma unroll
+      for (int u = 0; u < kWideAhead; ++u)
+        if (i0 + u * 64 < last) f(key[u], position[u], i0 + u * 64 + lane < last);
+    }
+  };
+  each([&](uint32_t key, uint32_t, bool live) {
+    if (live) __hip_atomic_fetch_add(&counters[wave][p.digit(key)], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  });
+  // this thread's digit in the tiles before, and in all
+  uint32_t before = 0, all = 0;
+#pragma unroll 8
+  for (int b = 0; b < p.tiles; ++b) {
+    const uint32_t c = p.counts[(int64_t)b * kWideThreads + t];
+    before += b < (int)blockIdx.x ? c : 0;
+    all += c;
+  }
+  uint32_t scan = all;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t o = __shfl_up(scan, d, 64);
+    if (lane >= d) scan += o;
+  }
+  if (lane == 63) sums[wave] = scan;
+  __syncthreads();
+  uint32_t base = scan - all + before;
+#pragma unroll
+  for (int w = 0; w < kWideWaves; ++w) base += w < wave ? sums[w] : 0;
+  // where each wave's words of the digit start
+#pragma unroll
+  for (int w = 0; w < kWideWaves; ++w) {
     const uint32_t c = counters[w][t];
     counters[w][t] = base;
     base += c;
   }
   __syncthreads();
-#pragma unroll
-  for (int r = 0; r < kTileRounds; ++r) {
-    const int64_t i = first + r * 64;
-    if (i >= p.T) continue;
-    const uint32_t to = counters[wave][p.digit(key[r])] + rank[r];
-    p.keys_out[to] = key[r];
-    p.positions_out[to] = p.tokens ? (uint32_t)i : p.positions[i];
-    if (p.used && key[r] < (uint32_t)p.V) {
-      const uint32_t high = key[r] >> kClassBits;
-      __hip_atomic_fetch_or(p.used + (key[r] & (kClasses - 1)) * used_words(p.V) + (high >> 5), 1u << (high & 31), __ATOMIC_RELAXED,
-                            __HIP_MEMORY_SCOPE_AGENT);
+  each([&](uint32_t key, uint32_t position, bool live) {
+    const uint32_t to = rank_in_wave<kWideDigit>(p.digit(key), live, counters[wave]);
+    if (live) {
+      p.keys_out[to] = key;
+      p.positions_out[to] = position;
     }
-  }
+  });
+}
+
+// The bitmap of the tokens that occur, from the sorted keys (the first of each run).
+__global__ __launch_bounds__(kThreads) void sort_mark_kernel(const uint32_t* keys, int64_t T, int64_t V, uint32_t* used) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= T) return;
+  const uint32_t key = keys[i], high = key >> kClassBits;
+  if (key >= (uint32_t)V || (i > 0 && keys[i - 1] == key)) return;
+  __hip_atomic_fetch_or(used + (key & (kClasses - 1)) * used_words(V) + (high >> 5), 1u << (high & 31), __ATOMIC_RELAXED,
+                        __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // ---- the sums -----------------------------------------------------------------------------
@@ -633,11 +640,12 @@ inline int64_t round16(int64_t n) { return (n + 15) / 16 * 16; }
 // The workspace's parts, in bytes from its start.
 struct Layout {
   int64_t keys[2], positions[2], counts, used, partials, bytes;
-  int tiles;
+  int tile, tiles;
   bool small;
   Layout(int64_t T, int64_t V, int64_t C) {
     small = T <= kSortMost && used_words(V) <= kUsedLds;
-    tiles = small ? 0 : (int)((T + kTile - 1) / kTile);
+    tile = small ? 0 : (int)tile_of(T);
+    tiles = small ? 0 : (int)((T + tile - 1) / tile);
     int64_t at = 0;
     auto take = [&](int64_t n) {
       const int64_t here = at;
@@ -707,14 +715,18 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t
       p.counts = words(l.counts);
       p.T = a.T;
       p.V = a.V;
+      p.tile = l.tile;
       p.tiles = l.tiles;
       p.shift = shift;
-      p.used = shift + kWideDigit >= bits ? words(l.used) : nullptr;
-      sort_count_kernel<<<l.tiles, kTileThreads, 0, s>>>(p);
+      p.used = shift == 0 && !a.accumulate ? words(l.used) : nullptr;
+      sort_count_kernel<<<l.tiles, kWideThreads, 0, s>>>(p);
       if ((e = hipGetLastError()) != hipSuccess) return e;
-      sort_scan_kernel<<<1, kSortThreads, 0, s>>>(p.counts, (int64_t)l.tiles << kWideDigit);
+      sort_move_kernel<<<l.tiles, kWideThreads, 0, s>>>(p);
       if ((e = hipGetLastError()) != hipSuccess) return e;
-      sort_move_kernel<<<l.tiles, kTileThreads, 0, s>>>(p);
+    }
+    if (!a.accumulate) {
+      sort_mark_kernel<<<(unsigned)((a.T + kThreads - 1) / kThreads), kThreads, 0, s>>>(words(l.keys[out]), a.T, a.V,
+                                                                                        words(l.used));
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
