@@ -11,9 +11,9 @@
 // leaves a sum per chunk in the workspace, and a second kernel adds those in order.  The rows of
 // tokens that do not occur are filled with zeros by a launch between the sort, which leaves a bitmap of
 // those that do, and the sums: most of what a whole gradient costs.  Bound by HBM, V C elements written
-// and T C read: 16384 tokens, 131072 x 4096 fp32 422 us, of them the sort 14, zeros 300 (7.1 TB/s), sums
-// 98 and their join 7.  Small tables wait for the chain of launches: 5003 tokens, 32000 x 2048 bf16, twice, 89
-// us (sorts 7, zeros 18, sums 10 and 14, joins 8) where the bytes would take 33.
+// and T C read: 16384 tokens, 131072 x 4096 fp32 409 us, of them the sort 13, zeros 303 (7.1 TB/s), sums
+// 84 and their join 6.  Small tables wait for the chain of launches: 5003 tokens, 32000 x 2048 bf16, twice, 77
+// us (sorts 7, zeros 18, sums 8 and 11, joins 7) where the bytes would take 33.
 #include "device_common.h"
 #include "rollout.h"
 
@@ -52,19 +52,26 @@ template <bool F32>
 __global__ __launch_bounds__(kThreads) void embedding_kernel(EmbeddingArgs a, int bands) {
   const int64_t t0 = (int64_t)(blockIdx.x / bands) * kLookupRows;
   const int64_t c = (int64_t)(blockIdx.x % bands) * kBand + threadIdx.x * 8;
+  // the rows' tokens, one a lane, in one load; -1: padding
+  const int lane = threadIdx.x & 63;
+  int64_t token = -1;
+  if (lane < kLookupRows && t0 + lane < a.T) token = a.tokens[t0 + lane];
+  const int index = token >= 0 && token < a.V ? (int)token : -1;
+  int v[kLookupRows];
+#pragma unroll
+  for (int i = 0; i < kLookupRows; ++i) v[i] = __builtin_amdgcn_readlane(index, i);
   if (c >= a.C) return;
   v4u p[kLookupRows], q[kLookupRows];
 #pragma unroll
   for (int i = 0; i < kLookupRows; ++i) {
-    const int64_t token = t0 + i < a.T ? a.tokens[t0 + i] : -1;
     p[i] = q[i] = v4u{0, 0, 0, 0};
-    if (token < 0 || token >= a.V) continue;
+    if (v[i] < 0) continue;
     if constexpr (F32) {
-      const v4u* const from = reinterpret_cast<const v4u*>(static_cast<const float*>(a.weight) + token * a.ldw + c);
+      const v4u* const from = reinterpret_cast<const v4u*>(static_cast<const float*>(a.weight) + v[i] * a.ldw + c);
       p[i] = from[0];
       q[i] = from[1];
     } else {
-      p[i] = *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(a.weight) + token * a.ldw + c);
+      p[i] = *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(a.weight) + v[i] * a.ldw + c);
     }
   }
 #pragma unroll
@@ -80,10 +87,8 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(EmbeddingArgs a, in
     } else {
       x.widen(p[i]);
     }
-    const int64_t token = a.tokens[t0 + i];
-    const bool live = token >= 0 && token < a.V;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = live ? x.v[e] * a.scale : 0.0f;
+    for (int e = 0; e < 8; ++e) x.v[e] = v[i] >= 0 ? x.v[e] * a.scale : 0.0f;
     *reinterpret_cast<v4u*>(a.y + (t0 + i) * a.ldy + c) = x.narrow();
   }
 }
@@ -303,7 +308,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(SmallSortArgs 
 
 // More tokens: a workgroup takes a tile of them, up to kTiles tiles, and a pass is two launches, the tiles'
 // counts by digit and the words to their places, where every workgroup adds up the counts before its own.
-// The first pass reads the tokens.  (WIDE_NOW.)
+// The first pass reads the tokens.  18888 tokens of 18212: two passes and the bitmap 23 us; with a third launch for
+// the counts' sums, tiles of 4096 and the bitmap from every token about 75.
 constexpr int kWideThreads = 512, kWideWaves = 8, kWideDigit = 9, kWideAhead = 4;
 static_assert(kWideThreads == 1 << kWideDigit);  // (thread d has digit d)
 constexpr int64_t kTiles = 128, kTileStep = 2 * kWideThreads;
@@ -482,44 +488,53 @@ __device__ __forceinline__ int64_t column(int64_t band) {
   return band * kBand + threadIdx.x * (F32 ? 4 : 8);
 }
 
+// As they are in memory: to be widened where they are used, so that a load waits for no other's.
 template <bool F32>
-__device__ __forceinline__ Eight load_dy(const uint16_t* row, bool second) {
-  Eight x;
+__device__ __forceinline__ v4u load_dy(const uint16_t* row, bool second) {
   if constexpr (F32) {
     const uint2 lo = *reinterpret_cast<const uint2*>(row);
     const uint2 hi = second ? *reinterpret_cast<const uint2*>(row + kHalf) : make_uint2(0, 0);
-    x.widen(v4u{lo.x, lo.y, hi.x, hi.y});
+    return v4u{lo.x, lo.y, hi.x, hi.y};
   } else {
-    x.widen(*reinterpret_cast<const v4u*>(row));
+    return *reinterpret_cast<const v4u*>(row);
   }
-  return x;
 }
 
 // What the columns of row v of the table from c on hold (second: the other four are inside it, too).
 template <bool F32>
-__device__ __forceinline__ Eight load_row(const EmbeddingBackwardArgs& a, uint32_t v, int64_t c, bool second) {
-  const int64_t at = (int64_t)v * a.ldw + c;
-  Eight x{};
-  if constexpr (F32) {
-    const float* const from = static_cast<const float*>(a.dweight) + at;
-    const v4u lo = *reinterpret_cast<const v4u*>(from);
-    const v4u hi = second ? *reinterpret_cast<const v4u*>(from + kHalf) : v4u{0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x.v[e] = __uint_as_float(lo[e]);
-      x.v[4 + e] = __uint_as_float(hi[e]);
+struct TableRow {
+  v4u p[F32 ? 2 : 1];
+  __device__ __forceinline__ void load(const EmbeddingBackwardArgs& a, uint32_t v, int64_t c, bool second) {
+    const int64_t at = (int64_t)v * a.ldw + c;
+    if constexpr (F32) {
+      const float* const from = static_cast<const float*>(a.dweight) + at;
+      p[0] = *reinterpret_cast<const v4u*>(from);
+      if (second) p[1] = *reinterpret_cast<const v4u*>(from + kHalf);
+    } else {
+      p[0] = *reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(a.dweight) + at);
     }
-  } else {
-    x.widen(*reinterpret_cast<const v4u*>(static_cast<const uint16_t*>(a.dweight) + at));
   }
-  return x;
-}
+  __device__ __forceinline__ Eight eight() const {
+    Eight x;
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x.v[e] = __uint_as_float(p[0][e]);
+        x.v[4 + e] = __uint_as_float(p[1][e]);
+      }
+    } else {
+      x.widen(p[0]);
+    }
+    return x;
+  }
+};
 
 template <bool F32, bool ADD>
 __device__ __forceinline__ void put_row(const EmbeddingBackwardArgs& a, uint32_t v, int64_t c, bool second,
-                                        const Eight& sum, const Eight& old) {
+                                        const Eight& sum, const TableRow<F32>& row) {
   const int64_t at = (int64_t)v * a.ldw + c;
-  Eight x;
+  Eight x, old{};
+  if (ADD) old = row.eight();
 #pragma unroll
   for (int e = 0; e < 8; ++e) x.v[e] = ADD ? old.v[e] + sum.v[e] * a.scale : sum.v[e] * a.scale;
   if constexpr (F32) {
@@ -538,51 +553,68 @@ __device__ __forceinline__ void put_row(const EmbeddingBackwardArgs& a, uint32_t
 }
 
 // A workgroup sums a chunk over a band of columns, kAhead positions at a time: their rows of dy
-// and, to be added to, the table's rows of the runs that end there are all in flight together.
+// and, to be added to, the table's rows of the runs that end there are all in flight together.  A wave reads the
+// keys and positions of 64 at once, one a lane, and has them as scalars from there: read one by one, each for
+// the whole wave, they and the rows waited for each other (40000 x 1024 bf16 68 us, so 37; 16384 x 4096 for an
+// fp32 table 98 and 84).
 constexpr int kChunk = 8;  // a chunk has a multiple of it
+constexpr int kAhead = 8;
 
 template <bool F32, bool ADD>
 __global__ __launch_bounds__(kThreads) void embedding_sums_kernel(Gradient g) {
   const EmbeddingBackwardArgs& a = g.a;
-  const int64_t j = blockIdx.x / g.bands, c = column<F32>(blockIdx.x % g.bands);
-  if (c >= a.C) return;
+  const int64_t j = blockIdx.x / g.bands;
+  int64_t c = column<F32>(blockIdx.x % g.bands);
+  const bool inside = c < a.C;
+  if (!__any(inside)) return;
+  if (!inside) c = 0;  // (lanes that store nothing)
   const bool second = !F32 || c + kHalf < a.C;
   const int64_t first = j * g.chunk, last = first + g.chunk < a.T ? first + g.chunk : a.T;
   float* const part = g.partials + j * 2 * a.C + c;
   const uint32_t V = (uint32_t)a.V;
+  const int lane = threadIdx.x & 63;
   bool from_before = first > 0 && g.keys[first - 1] == g.keys[first];
-  constexpr int kAhead = ADD ? 4 : 8;  // (eight with the rows that are added to: 152 registers, 160 us for 122)
   Eight sum{};
-  for (int64_t i0 = first; i0 < last; i0 += kAhead) {
-    Eight x[kAhead], old[kAhead];
-    uint32_t key[kAhead + 1];
+  for (int64_t block = first; block < last; block += 64) {
+    const int64_t i = block + lane;
+    const uint32_t keys = i < a.T ? g.keys[i] : 0xffffffffu, nexts = i + 1 < a.T ? g.keys[i + 1] : 0xffffffffu,
+                   positions = i < a.T ? g.positions[i] : 0;
+    const int n = last - block < 64 ? (int)(last - block) : 64;
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+      v4u x[kAhead];
+      TableRow<F32> old[kAhead];
+      uint32_t key[kAhead], next[kAhead];
 #pragma unroll
-    for (int u = 0; u <= kAhead; ++u) key[u] = i0 + u < a.T ? g.keys[i0 + u] : 0xffffffffu;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      x[u] = old[u] = Eight{};
-      if (key[u] < V) {
-        x[u] = load_dy<F32>(a.dy + (int64_t)g.positions[i0 + u] * a.lddy + c, second);
-        if (ADD && key[u + 1] != key[u]) old[u] = load_row<F32>(a, key[u], c, second);
+      for (int u = 0; u < kAhead; ++u) {
+        key[u] = __builtin_amdgcn_readlane(keys, i0 + u);
+        next[u] = __builtin_amdgcn_readlane(nexts, i0 + u);
+        x[u] = v4u{0, 0, 0, 0};
+        old[u] = TableRow<F32>{};
+        if (key[u] < V) {
+          x[u] = load_dy<F32>(a.dy + (int64_t)__builtin_amdgcn_readlane(positions, i0 + u) * a.lddy + c, second);
+          if (ADD && next[u] != key[u]) old[u].load(a, key[u], c, second);
+        }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (key[u] >= V) break;  // (the tokens outside come last)
+      for (int u = 0; u < kAhead; ++u) {
+        if (key[u] >= V) break;  // (the tokens outside come last)
+        Eight now;
+        now.widen(x[u]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum.v[e] += x[u].v[e];
-      const bool ends = key[u + 1] != key[u];
-      if (!ends && i0 + u + 1 != last) continue;
-      if (ends && !from_before) {
-        put_row<F32, ADD>(a, key[u], c, second, sum, old[u]);
-      } else {
-        float* const to = part + (from_before ? 0 : a.C);
-        *reinterpret_cast<float4*>(to) = make_float4(sum.v[0], sum.v[1], sum.v[2], sum.v[3]);
-        if (second)
-          *reinterpret_cast<float4*>(to + (F32 ? kHalf : 4)) = make_float4(sum.v[4], sum.v[5], sum.v[6], sum.v[7]);
+        for (int e = 0; e < 8; ++e) sum.v[e] += now.v[e];
+        const bool ends = next[u] != key[u];
+        if (!ends && block + i0 + u + 1 != last) continue;
+        if (inside && ends && !from_before) {
+          put_row<F32, ADD>(a, key[u], c, second, sum, old[u]);
+        } else if (inside) {
+          float* const to = part + (from_before ? 0 : a.C);
+          *reinterpret_cast<float4*>(to) = make_float4(sum.v[0], sum.v[1], sum.v[2], sum.v[3]);
+          if (second)
+            *reinterpret_cast<float4*>(to + (F32 ? kHalf : 4)) = make_float4(sum.v[4], sum.v[5], sum.v[6], sum.v[7]);
+        }
+        sum = Eight{};
+        from_before = false;
       }
-      sum = Eight{};
-      from_before = false;
     }
   }
 }
@@ -594,15 +626,24 @@ __global__ __launch_bounds__(kThreads) void embedding_join_kernel(Gradient g) {
   const EmbeddingBackwardArgs& a = g.a;
   const int64_t j = blockIdx.x / g.bands, c = column<F32>(blockIdx.x % g.bands);
   const int64_t next = (j + 1) * g.chunk;  // (below T: the last chunk has no next)
-  const uint32_t key = g.keys[next - 1], after = g.keys[next], before = j > 0 ? g.keys[j * g.chunk - 1] : 0xffffffffu;
+  // (three keys in one load: the chunk's last, the next one's first, and the one before the chunk; and beside
+  // it the first of each of 64 chunks, the next one on)
+  const int lane = threadIdx.x & 63;
+  const int64_t here = lane == 0 ? next - 1 : (lane == 1 ? next : j * g.chunk - 1);
+  const uint32_t three = here >= 0 ? g.keys[here] : 0xffffffffu;
+  const int64_t there = next + (int64_t)lane * g.chunk;
+  const uint32_t firsts = there < a.T ? g.keys[there] : 0xffffffffu;
+  const uint32_t key = __builtin_amdgcn_readlane(three, 0), after = __builtin_amdgcn_readlane(three, 1),
+                 before = __builtin_amdgcn_readlane(three, 2);
   if (key >= (uint32_t)a.V || after != key || before == key) return;  // none, or it started before
   // the chunks after j whose first position is the run's: those up to j + more
-  int more = 0;
-  for (int64_t base = next;; base += (int64_t)kThreads * g.chunk) {
-    const int64_t at = base + (int64_t)threadIdx.x * g.chunk;
-    const int n = __syncthreads_count(at < a.T && g.keys[at < a.T ? at : 0] == key);
+  int more = __popcll(__ballot(firsts == key));
+  for (int64_t base = next; more % 64 == 0;) {
+    base += (int64_t)64 * g.chunk;
+    const int64_t at = base + (int64_t)lane * g.chunk;
+    const int n = __popcll(__ballot(at < a.T && g.keys[at < a.T ? at : 0] == key));
     more += n;
-    if (n < kThreads) break;
+    if (n == 0) break;
   }
   if (c >= a.C) return;
   const bool second = !F32 || c + kHalf < a.C;
@@ -612,15 +653,16 @@ __global__ __launch_bounds__(kThreads) void embedding_join_kernel(Gradient g) {
     const float4 hi = second ? *reinterpret_cast<const float4*>(from + (F32 ? kHalf : 4)) : make_float4(0, 0, 0, 0);
     return Eight{{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}};
   };
-  Eight sum = load(part + a.C), old{};
-  if (ADD) old = load_row<F32>(a, key, c, second);
-  constexpr int kAhead = 16;
-  for (int i0 = 1; i0 <= more; i0 += kAhead) {
-    Eight x[kAhead];
+  Eight sum = load(part + a.C);
+  TableRow<F32> old{};
+  if (ADD) old.load(a, key, c, second);
+  constexpr int kParts = 16;
+  for (int i0 = 1; i0 <= more; i0 += kParts) {
+    Eight x[kParts];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) x[u] = load(part + (int64_t)(i0 + u <= more ? i0 + u : more) * 2 * a.C);
+    for (int u = 0; u < kParts; ++u) x[u] = load(part + (int64_t)(i0 + u <= more ? i0 + u : more) * 2 * a.C);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
+    for (int u = 0; u < kParts; ++u)
       if (i0 + u <= more)
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum.v[e] += x[u].v[e];
