@@ -21,7 +21,7 @@ def guarded(n, dtype=torch.uint8):
     return raw[:n * size].view(dtype), lambda: bool((raw[n * size:] == GUARD).all())
 
 
-@pytest.mark.parametrize("T", [1, 1024, 4096, 4097, 8192, 8193, 16384, 16385])
+@pytest.mark.parametrize("T", [1, 64, 256, 257, 1024, 4096, 4097, 8192, 8193, 16384, 16385])
 @pytest.mark.parametrize("step", [1, 64])
 def test_gradient_where_the_sort_changes(T, step):
     """step 64: all tokens in one class, with as many keys in it as it can have."""
