@@ -4,16 +4,17 @@
 //
 // A token outside 0 .. V-1 (padding) gives a row of zeros and takes no part in the gradient.
 //
-// The gradient sums each row in the order of t, in fp32, so that every run gives the same
-// bits.  Few tokens are compared with each other (embedding_few_kernel).  More: the tokens are sorted (stably: by token, then by t), the sorted positions are cut into
-// chunks, and a workgroup adds up the rows of dy of one chunk, over a band of columns, run by
-// run of equal tokens.  A run inside a chunk goes to the table at once; one that crosses chunks
-// leaves a sum per chunk in the workspace, and a second kernel adds those in order.  The rows of
-// tokens that do not occur are filled with zeros by a launch between the sort, which leaves a bitmap of
-// those that do, and the sums: most of what a whole gradient costs.  Bound by HBM, V C elements written
-// and T C read: 16384 tokens, 131072 x 4096 fp32 409 us, of them the sort 13, zeros 303 (7.1 TB/s), sums
-// 84 and their join 6.  Small tables wait for the chain of launches: 5003 tokens, 32000 x 2048 bf16, twice, 77
-// us (sorts 7, zeros 18, sums 8 and 11, joins 7) where the bytes would take 33.
+// The gradient sums each row in the order of t, in fp32, so that every run gives the same bits.
+// Up to kFewTokens tokens are compared with each other (embedding_few_kernel).  More are sorted
+// (stably: by token, then by t), the sorted positions are cut into chunks, and a workgroup adds up
+// the rows of dy of one chunk, over a band of columns, run by run of equal tokens.  A run inside a
+// chunk goes to the table at once; one that crosses chunks leaves a sum per chunk in the workspace,
+// and a second kernel adds those in order.  The rows of tokens that do not occur are filled with zeros by a
+// launch between the sort, which leaves a bitmap of those that do, and the sums: most of what a whole
+// gradient costs.  Bound by HBM, V C elements written and T C read: 16384 tokens, 131072 x 4096 fp32 409
+// us, of them the sort 13, zeros 303 (7.1 TB/s), sums 84 and their join 6.  Small tables wait for the chain of
+// launches: 5003 tokens, 32000 x 2048 bf16, twice, 77 us (sorts 7, zeros 18, sums 8 and 11, joins 7) where the
+// bytes would take 33.
 #include "device_common.h"
 #include "rollout.h"
 
