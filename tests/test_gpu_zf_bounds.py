@@ -93,3 +93,18 @@ def test_quantized(rows, cols):
     for a, b in zip(got, want):
         same(a, b, "given outputs")
     same(y[0].view(rows, cols), fp8q.dequantize_mx4(*want, cols), "values")
+
+
+@pytest.mark.parametrize("T", [300, 5000])
+def test_vocabulary_too_large_for_the_small_sort(T):
+    V, C = (1 << 21) + 64, 16
+    print("embedding gradient", T, V, flush=True)
+    g = torch.Generator().manual_seed(T)
+    t = torch.randint(V - 400, V + 20, (T,), generator=g)
+    t[::7] = torch.randint(0, V, (t[::7].numel(),), generator=g)
+    dy = torch.randn(T, C, generator=g).bfloat16()
+    got = fp8q.embedding_backward(dy.to(DEV), t.to(DEV), V, 2.0)
+    check_gradient(got, dy, t, V, 2.0, torch.float32, what="large vocabulary")
+    old = torch.randn(V, C, generator=g)
+    into = fp8q.embedding_backward(dy.to(DEV), t.to(DEV), V, 2.0, dweight=old.to(DEV), accumulate=True)
+    check_gradient(into, dy, t, V, 2.0, torch.float32, old=old, what="added")
