@@ -144,7 +144,7 @@ fp8q_status fp8q_embedding(const void* weight, fp8q_dtype dtype, int64_t V, int6
 int64_t fp8q_embedding_backward_workspace(int64_t T, int64_t V, int64_t C) {
   if (T <= 0 || V <= 0 || C <= 0 || T > kMaxRows || !dims_ok(V, C) || C % 16 || V * C >= ((int64_t)1 << 33)) return -1;
   // (launches of less than 2^32 threads: a thread of the zeros 16 bytes, a workgroup of the sums eight
-  // tokens or more by a band of 2048 columns)
+  // tokens or more by a band of 2048 columns; of one token only where that is less, too, see takes_few)
   if (T * ((C + 2047) / 2048) > ((int64_t)1 << 25)) return -1;
   return fp8q::embedding_backward_workspace(T, V, C);
 }

@@ -732,10 +732,17 @@ __global__ __launch_bounds__(kThreads) void embedding_few_kernel(Gradient g) {
   if (inside) put_row<F32, ADD>(a, key, c, second, sum, old);
 }
 
+inline int64_t bands_of(int64_t C) { return (C + kBand - 1) / kBand; }
+
+// Whether tokens are compared and not sorted: few of them, in rows whose bands leave the launch's threads below 2^32.
+inline bool takes_few(int64_t T, int64_t C) {
+  return T <= kFewTokens && T * bands_of(C) < ((int64_t)1 << 32) / kThreads;
+}
+
 // Positions of a chunk, a multiple of kChunk: more where that leaves 2048 workgroups or more.
 inline int chunk_of(int64_t T, int64_t C) {
   int64_t n = kChunk;
-  while (n * 2048 <= T * ((C + kBand - 1) / kBand) && n < ((int64_t)1 << 20)) n *= 2;
+  while (n * 2048 <= T * bands_of(C) && n < ((int64_t)1 << 20)) n *= 2;
   return (int)n;
 }
 
@@ -780,7 +787,7 @@ inline int bits_of(int64_t V) {  // of the keys 0 .. V
 using namespace embedding_detail;
 
 hipError_t launch_embedding(const EmbeddingArgs& a, hipStream_t s) {
-  const int bands = (int)((a.C + kBand - 1) / kBand);
+  const int bands = (int)bands_of(a.C);
   const unsigned grid = (unsigned)((a.T + kLookupRows - 1) / kLookupRows * bands);
   if (a.f32)
     embedding_kernel<true><<<grid, kThreads, 0, s>>>(a, bands);
@@ -792,7 +799,7 @@ hipError_t launch_embedding(const EmbeddingArgs& a, hipStream_t s) {
 int64_t embedding_backward_workspace(int64_t T, int64_t V, int64_t C) { return Layout(T, V, C).bytes; }
 
 hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t s) {
-  const int bands = (int)((a.C + kBand - 1) / kBand);
+  const int bands = (int)bands_of(a.C);
   Gradient g;
   g.a = a;
   g.bands = bands;
@@ -807,7 +814,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t
     return hipGetLastError();
   };
   hipError_t e;
-  if (a.T <= kFewTokens) {
+  if (takes_few(a.T, a.C)) {
     g.used = nullptr;
     if ((e = fill()) != hipSuccess) return e;
     const unsigned grid = (unsigned)(a.T * bands);
