@@ -796,7 +796,10 @@ hipError_t launch_embedding(const EmbeddingArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-int64_t embedding_backward_workspace(int64_t T, int64_t V, int64_t C) { return Layout(T, V, C).bytes; }
+// (tokens that are compared leave nothing in it: one piece, so that it has an address)
+int64_t embedding_backward_workspace(int64_t T, int64_t V, int64_t C) {
+  return takes_few(T, C) ? 16 : Layout(T, V, C).bytes;
+}
 
 hipError_t launch_embedding_backward(const EmbeddingBackwardArgs& a, hipStream_t s) {
   const int bands = (int)bands_of(a.C);

@@ -118,6 +118,15 @@ def test_gradient_paths(launches):
         assert status == 0 and ("embedding_few_kernel" in names) == few and ("sort_" in names) != few, (T, V, C, names)
 
 
+def test_gradient_workspace():
+    """Tokens that are compared need none to speak of; one token more never needs less."""
+    need = fp8q.lib().fp8q_embedding_backward_workspace
+    for V, C in ((1, 16), (131072, 4096), (1 << 20, 8176), (1, 1 << 27)):
+        sizes = [need(T, V, C) for T in (1, 8, 127, 255, 256, 257, 300)]
+        assert sizes == sorted(sizes) and sizes[0] == 16 and all(n > 0 for n in sizes)
+        assert (sizes[4] == 16) == (C < 1 << 27) and sizes[5] > 257 * 8
+
+
 def test_rows(launches):
     calls = [embedding(T, V, C, f32) for T, V, C in ((1, 1, MOST - 15), (4, MOST, 16), (32, 9, MOST - 15), ((1 << 22) - 1, 9, 16384),
                                                      (1 << 14, 9, 1 << 22)) for f32 in (0, 1)]
