@@ -818,6 +818,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint8_t* lds_all, i
   // (1x128 x 1x128: the column scales, two row scales and a fragment at most)
   constexpr int kScaleReads = PAIR == kPairBlock ? TI + (GATED ? 2 : 1) : 0;
   static_assert((PAIR == kPairBlockK ? TJ + 2 : kScaleReads) + 2 <= 15, "outstanding LDS reads must fit the lgkm counter");
+  // (E2M1: TJ + 1 scale pairs and TJ + 1 fragments of two reads each)
+  static_assert(PAIR != kPairMx4 || 3 * (TJ + 1) <= 15, "the LDS reads of an MXFP4 step before its first wait must fit the lgkm counter");
 
   // One K step; kMore: the loads of stage kt + kStages - 1 go out during
   // it (all but the last kStages - 1 steps, which run without, so that no
