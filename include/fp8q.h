@@ -681,10 +681,11 @@ fp8q_status fp8q_dequantize_mx4(const uint8_t *codes, int64_t ldc,
  *   A, sA  codes [M][lda] and scales of M rows of K elements; B, sB of N rows
  *   C      bf16 [M][ldc]
  * K counts codes, zeros past a row's end among them: a multiple of 256; M and N are free.
- * lda, ldb in bytes, at least K / 2.  M K / 32 and N K / 32 below 2^31 (else
- * FP8Q_ERR_UNSUPPORTED).  Alignment: A and B 16-byte aligned, lda % 16 == 0, ldb % 16 == 0;
- * sA and sB 8-byte aligned; C 8-byte aligned with ldc % 4 == 0.  Results are the same on
- * every run.
+ * lda, ldb in bytes, at least K / 2.  M K / 32 and N K / 32 below 2^31, lda below 2^23,
+ * ldb below 2^20 (so K below 2^21), ldc below 2^22, and up to 2^22 tiles of 128 x 128 of C
+ * (else FP8Q_ERR_UNSUPPORTED).  Alignment: A and B 16-byte aligned, lda % 16 == 0, ldb % 16
+ * == 0; sA and sB 8-byte aligned; C 8-byte aligned with ldc % 4 == 0.  Results are the same
+ * on every run.
  */
 fp8q_status fp8q_gemm_mx4(const uint8_t *A, const uint8_t *sA, int64_t lda,
                           const uint8_t *B, const uint8_t *sB, int64_t ldb,
@@ -694,9 +695,10 @@ fp8q_status fp8q_gemm_mx4(const uint8_t *A, const uint8_t *sA, int64_t lda,
 /*
  * Rows of an embedding table for T tokens: y[t] = scale weight[token], bf16 [T][ldy],
  * rounded once from fp32; weight [V][ldw], bf16 or fp32 (dtype).  A token outside
- * 0 .. V-1 (padding) gives a row of zeros.  Shape rules: C % 16 == 0, T below 2^22
- * (else FP8Q_ERR_UNSUPPORTED).  Alignment: weight and y 16-byte aligned, ldy % 8 == 0, ldw % 8
- * == 0 (fp32: % 4); tokens 8-byte.  scale finite (else FP8Q_ERR_INVAL).
+ * 0 .. V-1 (padding) gives a row of zeros.  Shape rules: C % 16 == 0, T below 2^22,
+ * ceil(T / 4) ceil(C / 2048) up to 2^23 (else FP8Q_ERR_UNSUPPORTED).  Alignment: weight and y
+ * 16-byte aligned, ldy % 8 == 0, ldw % 8 == 0 (fp32: % 4); tokens 8-byte.  scale finite (else
+ * FP8Q_ERR_INVAL).
  */
 fp8q_status fp8q_embedding(const void *weight, fp8q_dtype dtype, int64_t V,
                            int64_t C, int64_t ldw, const int64_t *tokens,
@@ -720,8 +722,8 @@ enum { FP8Q_ACCUMULATE = 32u };
  * 0 .. V-1 take no part (their rows of dy are not read).
  * workspace: at least fp8q_embedding_backward_workspace(T, V, C) bytes, 16-byte aligned,
  * overwritten (calls that share one must be ordered).  Shape rules: C % 16 == 0, T below 2^22,
- * V C below 2^33, T ceil(C / 2048) up to 2^25 (else FP8Q_ERR_UNSUPPORTED).  Alignment: as fp8q_embedding.  dweight must not
- * overlap dy.
+ * V C below 2^33, T ceil(C / 2048) up to 2^25 (else FP8Q_ERR_UNSUPPORTED).  Alignment: as
+ * fp8q_embedding.  dweight must not overlap dy.
  */
 fp8q_status fp8q_embedding_backward(const void *dy, int64_t lddy,
                                     const int64_t *tokens, int64_t T, int64_t V,

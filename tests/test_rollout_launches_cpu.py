@@ -83,8 +83,8 @@ def dequantize(rows, cols):
     return ("fp8q_dequantize_mx4", [AT, P // 2, AT, rows, cols, AT, cols, 0])
 
 
-def gemm(M, N, K, ldc=None):
-    return ("fp8q_gemm_mx4", [AT, AT, K // 2, AT, AT, K // 2, M, N, K, AT, ldc or wide(N), 0])
+def gemm(M, N, K, lda=None, ldb=None, ldc=None):
+    return ("fp8q_gemm_mx4", [AT, AT, lda or K // 2, AT, AT, ldb or K // 2, M, N, K, AT, ldc or wide(N), 0])
 
 
 def check(calls, results):
@@ -150,3 +150,39 @@ def test_products(launches):
                                 (1 << 15, 1 << 15, 1 << 20), (65536, 4, (1 << 20) - 256), ((1 << 28) - 128, 128, 256),
                                 (4, 65535, (1 << 20) - 256), (3001, 17408, 5120))]
     check(calls, launches(calls))
+
+
+UNSUPPORTED = -2
+HEADER = os.path.join(os.path.dirname(HERE), "include", "fp8q.h")
+
+
+def rules(name):
+    """What the header says before the declaration of `name`, in one line."""
+    text = open(HEADER).read()
+    at = text.index("fp8q_status %s(" % name)
+    return " ".join(text[text.rindex("/*", 0, at):at].replace("\n *", " ").split())
+
+
+# (taken, refused, the rule as the header states it)
+LIMITS = [
+    (gemm(128, 128, 1 << 20, lda=(1 << 23) - 16), gemm(128, 128, 1 << 20, lda=1 << 23), "lda below 2^23"),
+    (gemm(128, 128, (1 << 21) - 256, ldb=(1 << 20) - 16), gemm(128, 128, 512, ldb=1 << 20), "ldb below 2^20 (so K below 2^21)"),
+    (gemm(128, 128, (1 << 21) - 256), gemm(128, 128, 1 << 21), "ldb below 2^20 (so K below 2^21)"),
+    (gemm(128, 128, 512, ldc=(1 << 22) - 4), gemm(128, 128, 512, ldc=1 << 22), "ldc below 2^22"),
+    (gemm(1 << 18, 1 << 18, 256), gemm(1 << 18, (1 << 18) + 1, 256), "up to 2^22 tiles of 128 x 128"),
+    (gemm((1 << 28) - 1, 1, 256), gemm(1 << 28, 1, 256), "M K / 32 and N K / 32 below 2^31"),
+    (embedding(1 << 14, 9, 1 << 22), embedding((1 << 14) + 1, 9, 1 << 22), "ceil(T / 4) ceil(C / 2048) up to 2^23"),
+    (embedding((1 << 22) - 1, 9, 16), embedding(1 << 22, 9, 16), "T below 2^22"),
+    (backward(1 << 20, 1, 1 << 16), backward(1 << 20, 1, (1 << 16) + 16), "T ceil(C / 2048) up to 2^25"),
+    (backward(5, (1 << 29) - 1, 16), backward(5, 1 << 29, 16), "V C below 2^33"),
+    (quantize(32 << 23, 512), quantize((32 << 23) + 1, 512), "Up to 2^23 tiles of 32 x 512"),
+]
+
+
+def test_limits(launches):
+    """The header's limits are the code's, on both sides, and a refused call launches nothing."""
+    results = launches([c for taken, refused, _ in LIMITS for c in (taken, refused)])
+    for i, (taken, refused, rule) in enumerate(LIMITS):
+        check([taken], results[2 * i:2 * i + 1])
+        assert results[2 * i + 1] == (UNSUPPORTED, []), (refused, results[2 * i + 1])
+        assert rule in rules(taken[0]), (taken[0], rule)
