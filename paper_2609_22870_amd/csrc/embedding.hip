@@ -5,7 +5,7 @@
 // A token outside 0 .. V-1 (padding) gives a row of zeros and takes no part in the gradient.
 //
 // The gradient sums each row in the order of t, in fp32, so that every run gives the same bits.
-// Up to kFewTokens tokens are compared with each other (embedding_few_kernel).  More are sorted
+// Up to kFewTokens tokens are compared with each other (embedding_few_kernel, see takes_few).  More are sorted
 // (stably: by token, then by t), the sorted positions are cut into chunks, and a workgroup adds up
 // the rows of dy of one chunk, over a band of columns, run by run of equal tokens.  A run inside a
 // chunk goes to the table at once; one that crosses chunks leaves a sum per chunk in the workspace,
@@ -14,7 +14,7 @@
 // gradient costs.  Bound by HBM, V C elements written and T C read: 16384 tokens, 131072 x 4096 fp32 409
 // us, of them the sort 13, zeros 303 (7.1 TB/s), sums 84 and their join 6.  Small tables wait for the chain of
 // launches: 5003 tokens, 32000 x 2048 bf16, twice, 77 us (sorts 7, zeros 18, sums 8 and 11, joins 7) where the
-// bytes would take 33.
+// bytes would take 23.
 #include "device_common.h"
 #include "rollout.h"
 
@@ -457,8 +457,8 @@ struct Gradient {
 };
 
 // Zeros in the rows that no token names, in all without a bitmap: one 16-byte piece a thread, workgroup after workgroup
-// along the table (2 GiB at 6.7 TB/s; four pieces a thread 6.0, rows of a range a workgroup 5.8,
-// workgroups that stay 4.9 to 5.8).
+// along the table (2 GiB 303 us, 7.1 TB/s; in a probe, back to back with the gaps between launches, 319, four
+// pieces a thread 363, workgroups that stay 378 to 433).
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void embedding_fill_kernel(Gradient g) {
   const EmbeddingBackwardArgs& a = g.a;
@@ -739,7 +739,8 @@ inline bool takes_few(int64_t T, int64_t C) {
   return T <= kFewTokens && T * bands_of(C) < ((int64_t)1 << 32) / kThreads;
 }
 
-// Positions of a chunk, a multiple of kChunk: more where that leaves 2048 workgroups or more.
+// Positions of a chunk, kChunk or a power of two times it: doubled while as many as they are make 2048 workgroups or
+// more, so that 1024 to 2047 are left (fewer where there were fewer, or at the most positions of a chunk).
 inline int chunk_of(int64_t T, int64_t C) {
   int64_t n = kChunk;
   while (n * 2048 <= T * bands_of(C) && n < ((int64_t)1 << 20)) n *= 2;

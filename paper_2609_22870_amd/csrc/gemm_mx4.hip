@@ -4,8 +4,10 @@
 // The kernels are those of gemm_tile.h: a K step is the 128 bytes that an FP8 step is, but
 // 256 codes, two instructions of half an FP8 one's time.
 //
-// Large products are bound by power: 16384 x 4096 x 12288 385 us, 4.3 PFLOP/s, at a clock of 1.63 to 1.66
-// GHz (operands of zeros 322; the matrix instructions alone reach 8.3 PFLOP/s).  Few rows are bound
+// Large products are bound by the way from LDS to the matrix units, then by power: 16384 x 4096 x 12288 385 to
+// 415 us, 4.0 to 4.3 PFLOP/s, with the matrix units busy in half of the cycles.  Of 8192^3 the matrix
+// instructions alone take 132 us (8.3 PFLOP/s), with the fragments' LDS reads 190, the whole kernel 197 on operands of
+// zeros and 240 on normal values: as many cycles, at 1.86 GHz in place of 2.29.  Few rows are bound
 // by the bytes that a CU loads, about 85 KB a us: 8 x 4096 x 12288 6.0 us (4.5 TB/s of weights), 64 x
 // 17408 x 5120 13.4 (3.7 TB/s).
 #include "gemm_tile.h"

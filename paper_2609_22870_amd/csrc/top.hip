@@ -222,8 +222,8 @@ __device__ __forceinline__ void select_top(Selection<THREADS, SLOTS>& s, const R
 
 // The sums of pieces first + t + i THREADS below last and of this thread's edge; NV in flight.
 // Chunks that are nothing but padding for the whole workgroup are left out (64 x 131072 bf16 15.1
-// -> 13.5 us, 2048 x 8000 fp32 22.2 -> 20.0; where none is, up to 2% for the test; workgroups of 1024 have rows
-// that fill them and lost as much).
+// -> 13.5 us of kernels, 16.8 -> 15.2 a pass, 2048 x 8000 fp32 22.2 -> 20.0 a pass; where none is, up to 2% for
+// the test; workgroups of 1024 have rows that fill them and lost as much).
 template <bool F32, int THREADS, int NV>
 __device__ __forceinline__ Sums own_sums(const Row<F32>& x, int first, int last, int edge, float c) {
   using P = Piece<F32>;
